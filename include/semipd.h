@@ -358,6 +358,41 @@ int spd_ffn_gate_up(spd_ctx* ctx, int phase, const void* x, const void* w_gu, vo
 int spd_ffn_pack_gate_up(spd_ctx* ctx, int phase, const void* w_gate, const void* w_up, void* w_gu, int32_t hidden,
                          int32_t inter);
 
+/* ------------------------------------------------------------------ the FFN in 8 and 4 bits
+ * Paper, Evaluation "Model": DeepSeek-V3 is served in FP8; the paper gives no scheme.  The formats taken here are the OCP microscaling ones: a
+ * block of 32 consecutive entries shares one scale 2^(b - 127), b a byte (E8M0), under which the entries are E4M3 (MXFP8) or E2M1 (MXFP4).  b is
+ * the smallest, and at least 1, with which the block's largest finite magnitude does not pass the format's largest value (448; 6); codes
+ * are rounded to nearest even. */
+
+/* RMS norm, with the addition of the residual stream ahead of it (the step ahead of either half of a layer of the Llama models):
+ *     h = bf16(x + residual), residual <- h (residual NULL: h = x),     y_i = h_i weight_i / sqrt(mean_j h_j^2 + eps)
+ * sums and products in fp32 (entries of a magnitude whose squares pass fp32's range are not meant).
+ * x, residual device [n_tokens, hidden], weight device [hidden], bf16.  With out_scales NULL, out is device [n_tokens, hidden] bf16 (nearest
+ * even) and hidden a multiple of 8.  Else out is device [n_tokens, hidden] bytes, the E4M3 codes of y (infinities and NaN: NaN), and out_scales
+ * device [hidden / 128][n_tokens][4] bytes, the scale of entries 128 a + 32 b .. + 31 of row t at [a][t][b]: the form that
+ * spd_ffn_gate_up_mx reads; hidden a multiple of 128.  hidden <= 32768; eps positive and finite; n_tokens >= 0 (0: nothing is enqueued).
+ * 16-byte aligned (out_scales: 4).  `out` may be x itself in the bf16 form; otherwise the buffers do not overlap.  Enqueued on `phase`'s current
+ * stream, as spd_ffn_gate_up is.  SPD_EINVAL on any violated condition, nothing enqueued. */
+int spd_rmsnorm(spd_ctx* ctx, int phase, const void* x, void* residual, const void* weight, float eps, void* out, void* out_scales,
+                int32_t n_tokens, int32_t hidden);
+
+/* The gated FFN's first step (spd_ffn_gate_up) over weights in MXFP4 and rows in MXFP8: the same products and activation on the values that codes
+ * and scales stand for, fp32 sums, one rounding to bf16 (nearest even).  17 / 32 byte per weight is read instead of 2.
+ * x device [n_tokens, hidden] E4M3 codes, x_scales device [hidden / 128][n_tokens][4] (as spd_rmsnorm writes them), w_mx device, of
+ * spd_ffn_mx_bytes bytes, as spd_ffn_pack_gate_up_mx writes it (its order is private to the library), out device [n_tokens, inter] row-major,
+ * bf16.  hidden and inter multiples of 128; x and w_mx 16-byte aligned, x_scales 4; n_tokens >= 0 (0: nothing is enqueued).  A NaN in a row
+ * of x makes that row of out NaN, a block of weights that is NaN its column.  Enqueued on `phase`'s current stream; the buffers
+ * belong to the caller and must stay valid until the stream has run the call.  SPD_EINVAL on any violated condition, nothing enqueued. */
+int spd_ffn_gate_up_mx(spd_ctx* ctx, int phase, const void* x, const void* x_scales, const void* w_mx, void* out, int32_t n_tokens, int32_t hidden,
+                       int32_t inter);
+/* Bytes of the packed weights: inter / 128 * hidden / 128 * 17408. */
+int spd_ffn_mx_bytes(int32_t hidden, int32_t inter, uint64_t* bytes_out);
+/* Quantises w_gate, w_up device [inter, hidden] row-major (bf16, 16-byte aligned) into w_mx (once per layer at load time).  A block of 32
+ * hidden entries with an infinity or NaN becomes NaN as a whole (scale byte 255). */
+int spd_ffn_pack_gate_up_mx(spd_ctx* ctx, int phase, const void* w_gate, const void* w_up, void* w_mx, int32_t hidden, int32_t inter);
+/* The values that w_mx stands for (exact in bf16), to w_gate, w_up.  For tests and for moving weights elsewhere. */
+int spd_ffn_unpack_gate_up_mx(spd_ctx* ctx, int phase, const void* w_mx, void* w_gate, void* w_up, int32_t hidden, int32_t inter);
+
 /* A decode worker inside the library (paper, System Design, "Prefill and Decode Workers": the
  * decode worker runs its iterations asynchronously beside the prefill worker).  Starts a host
  * thread that calls spd_decode_step on batches[0], batches[1], ... batches[n_batches-1],

@@ -1,0 +1,126 @@
+// RMS norm with the residual's addition, and an output in bf16 or in 8 bits with scales.
+//
+// For a row x of `hidden` entries (and the residual stream's row r, where there is one):
+//     h = bf16(x + r),  r <- h,      y_i = h_i w_i / sqrt(mean_j h_j^2 + eps)
+// in fp32, y rounded once: to bf16, or to MX E4M3 (mx.h: blocks of 32 entries under one power-of-two scale).
+//
+// Bound by memory: every row is read once and written once.  A workgroup takes a row and keeps it in registers between the sum of squares
+// and the output; the block maxima of the 8-bit form are formed over the four lanes that hold a block.
+#include "mx.h"
+
+#include <algorithm>
+
+namespace spd {
+
+namespace {
+typedef unsigned short bf16_t;
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+__device__ inline uint32_t pack_bf16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+__device__ inline float bf_lo(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
+__device__ inline float bf_hi(uint32_t w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
+
+struct NormArgs {
+  const bf16_t* x;
+  bf16_t* residual;
+  const bf16_t* w;
+  void* out;
+  uint32_t* scales;                                // [hidden / 128][T]: the four scale bytes of 128 entries
+  float eps;
+  int T, hidden;
+  StepMark mark;
+};
+}  // namespace
+
+// grid (T), block THREADS: a row of up to THREADS * PIECES pieces of 8 entries
+template <int THREADS, int PIECES, bool MX>
+__global__ __launch_bounds__(THREADS) void rmsnorm_kernel(NormArgs a) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) store_mark(a.mark);
+  const int tid = threadIdx.x, n = a.hidden >> 3, t = blockIdx.x;
+  const size_t row = (size_t)t * a.hidden;
+  uint4 h[PIECES];
+  float sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < PIECES; ++j) {
+    const int p = tid + THREADS * j;
+    h[j] = uint4{0, 0, 0, 0};
+    if (p < n) {
+      h[j] = *(const uint4*)(a.x + row + 8 * p);
+      if (a.residual) {
+        const uint4 r = *(const uint4*)(a.residual + row + 8 * p);
+        uint32_t hw[4] = {h[j].x, h[j].y, h[j].z, h[j].w};
+        const uint32_t rw[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) hw[i] = pack_bf16(bf_lo(hw[i]) + bf_lo(rw[i]), bf_hi(hw[i]) + bf_hi(rw[i]));
+        h[j] = uint4{hw[0], hw[1], hw[2], hw[3]};
+        *(uint4*)(a.residual + row + 8 * p) = h[j];
+      }
+    }
+    const uint32_t hw[4] = {h[j].x, h[j].y, h[j].z, h[j].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sum = __builtin_fmaf(bf_lo(hw[i]), bf_lo(hw[i]), sum);
+      sum = __builtin_fmaf(bf_hi(hw[i]), bf_hi(hw[i]), sum);
+    }
+  }
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) sum += __shfl_xor(sum, s);
+  if constexpr (THREADS > 64) {
+    __shared__ float part[THREADS / 64];
+    if ((tid & 63) == 0) part[tid >> 6] = sum;
+    __syncthreads();
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < THREADS / 64; ++i) sum += part[i];
+  }
+  const float inv = 1.f / sqrtf(sum / (float)a.hidden + a.eps);
+#pragma unroll
+  for (int j = 0; j < PIECES; ++j) {
+    const int p = tid + THREADS * j;
+    if (p >= n) break;                             // (in the 8-bit form whole groups of 16 lanes leave together)
+    const uint4 wv = *(const uint4*)(a.w + 8 * p);
+    const uint32_t hw[4] = {h[j].x, h[j].y, h[j].z, h[j].w}, ww[4] = {wv.x, wv.y, wv.z, wv.w};
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y[2 * i] = bf_lo(hw[i]) * inv * bf_lo(ww[i]);
+      y[2 * i + 1] = bf_hi(hw[i]) * inv * bf_hi(ww[i]);
+    }
+    if constexpr (!MX) {
+      *(uint4*)((bf16_t*)a.out + row + 8 * p) = uint4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
+    } else {
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = max(m, finite_magnitude(y[i]));
+      m = max(m, (uint32_t)__shfl_xor((int)m, 1));
+      m = max(m, (uint32_t)__shfl_xor((int)m, 2));
+      const uint32_t b = scale_byte_e4m3(m);
+      const float f = inverse_scale_of(b);
+      *(uint2*)((char*)a.out + row + 8 * p) = uint2{e4m3_codes(y[0] * f, y[1] * f, y[2] * f, y[3] * f), e4m3_codes(y[4] * f, y[5] * f, y[6] * f, y[7] * f)};
+      uint32_t four = b << (8 * ((tid >> 2) & 3));
+      four |= (uint32_t)__shfl_xor((int)four, 4);
+      four |= (uint32_t)__shfl_xor((int)four, 8);
+      if ((tid & 15) == 0) a.scales[(size_t)(p >> 4) * a.T + t] = four;
+    }
+  }
+}
+
+hipError_t launch_rmsnorm(const void* x, void* residual, const void* weight, float eps, void* out, void* out_scales, int T, int hidden, int cus,
+                          const StepMark& mark, hipStream_t stream) {
+  (void)cus;
+  NormArgs a{(const bf16_t*)x, (bf16_t*)residual, (const bf16_t*)weight, out, (uint32_t*)out_scales, eps, T, hidden, mark};
+  auto launch = [&](auto mx, auto bf, int threads) { hipLaunchKernelGGL(out_scales ? mx : bf, dim3((unsigned)T), dim3((unsigned)threads), 0, stream, a); };
+  const int n = hidden / 8;
+  if (n <= 64) launch(rmsnorm_kernel<64, 1, true>, rmsnorm_kernel<64, 1, false>, 64);
+  else if (n <= 256) launch(rmsnorm_kernel<256, 1, true>, rmsnorm_kernel<256, 1, false>, 256);
+  else if (n <= 512) launch(rmsnorm_kernel<256, 2, true>, rmsnorm_kernel<256, 2, false>, 256);
+  else if (n <= 1024) launch(rmsnorm_kernel<256, 4, true>, rmsnorm_kernel<256, 4, false>, 256);
+  else if (n <= 2048) launch(rmsnorm_kernel<1024, 2, true>, rmsnorm_kernel<1024, 2, false>, 1024);
+  else launch(rmsnorm_kernel<1024, 4, true>, rmsnorm_kernel<1024, 4, false>, 1024);
+  return hipGetLastError();
+}
+
+}  // namespace spd

@@ -33,6 +33,7 @@ EXPORTS = [
     "spd_decode_worker_start", "spd_decode_worker_stop", "spd_decode_worker_steps",
     "spd_ctrl_create", "spd_ctrl_destroy", "spd_ctrl_observe_ttft", "spd_ctrl_observe_tpot", "spd_ctrl_step", "spd_ctrl_model",
     "spd_rope_inv_freq", "spd_rope_qk", "spd_ffn_gate_up", "spd_ffn_pack_gate_up",
+    "spd_rmsnorm", "spd_ffn_mx_bytes", "spd_ffn_pack_gate_up_mx", "spd_ffn_unpack_gate_up_mx", "spd_ffn_gate_up_mx",
     "spd_decode_step_noalloc", "spd_noalloc_limits", "spd_phase_read", "spd_phase_read_lds", "spd_clock_probe", "spd_issue_probe",
     "spd_shm_pool_create", "spd_shm_pool_open", "spd_shm_pool_close", "spd_shm_pool_unlink", "spd_shm_pool_stats",
     "spd_shm_kv_reserve", "spd_shm_kv_free", "spd_shm_kv_block_table", "spd_shm_kv_free_list",
@@ -138,6 +139,11 @@ def _load() -> C.CDLL:
         "spd_rope_qk": [vp, C.c_int, P(spd_rope_config), P(i32), i32, vp, i32, vp, i32, i32],
         "spd_ffn_gate_up": [vp, C.c_int, vp, vp, vp, i32, i32, i32],
         "spd_ffn_pack_gate_up": [vp, C.c_int, vp, vp, vp, i32, i32],
+        "spd_rmsnorm": [vp, C.c_int, vp, vp, vp, C.c_float, vp, vp, i32, i32],
+        "spd_ffn_mx_bytes": [i32, i32, P(u64)],
+        "spd_ffn_pack_gate_up_mx": [vp, C.c_int, vp, vp, vp, i32, i32],
+        "spd_ffn_unpack_gate_up_mx": [vp, C.c_int, vp, vp, vp, i32, i32],
+        "spd_ffn_gate_up_mx": [vp, C.c_int, vp, vp, vp, vp, i32, i32, i32],
         "spd_shm_pool_create": [C.c_char_p, i64, i32, i32, P(vp)],
         "spd_shm_pool_open": [C.c_char_p, P(vp)],
         "spd_shm_pool_close": [vp],
@@ -315,6 +321,22 @@ class Context:
         """The joint matrix [2 inter, hidden] (blocks of 32 gate rows + their 32 up rows) from the two weight matrices."""
         _check(lib.spd_ffn_pack_gate_up(self.h, phase, _ptr(w_gate), _ptr(w_up), _ptr(w_gu), hidden, inter), "spd_ffn_pack_gate_up")
 
+    def rmsnorm(self, phase: int, x, residual, weight, eps: float, out, n_tokens: int, hidden: int, out_scales=None) -> None:
+        """residual <- bf16(x + residual) (None: x as it is); out = its RMS norm times weight: bf16, or with out_scales E4M3 codes."""
+        _check(lib.spd_rmsnorm(self.h, phase, _ptr(x), _ptr(residual), _ptr(weight), eps, _ptr(out), _ptr(out_scales), n_tokens, hidden), "spd_rmsnorm")
+
+    def ffn_pack_gate_up_mx(self, phase: int, w_gate, w_up, w_mx, hidden: int, inter: int) -> None:
+        """The MXFP4 weights (ffn_mx_bytes bytes) of the two bf16 matrices [inter, hidden]."""
+        _check(lib.spd_ffn_pack_gate_up_mx(self.h, phase, _ptr(w_gate), _ptr(w_up), _ptr(w_mx), hidden, inter), "spd_ffn_pack_gate_up_mx")
+
+    def ffn_unpack_gate_up_mx(self, phase: int, w_mx, w_gate, w_up, hidden: int, inter: int) -> None:
+        """The values that MXFP4 weights stand for, to two bf16 matrices [inter, hidden]."""
+        _check(lib.spd_ffn_unpack_gate_up_mx(self.h, phase, _ptr(w_mx), _ptr(w_gate), _ptr(w_up), hidden, inter), "spd_ffn_unpack_gate_up_mx")
+
+    def ffn_gate_up_mx(self, phase: int, x, x_scales, w_mx, out, n_tokens: int, hidden: int, inter: int) -> None:
+        """out [T, inter] = silu(x W_gate^T) * (x W_up^T) from E4M3 rows with their scales (as rmsnorm writes them) and MXFP4 weights."""
+        _check(lib.spd_ffn_gate_up_mx(self.h, phase, _ptr(x), _ptr(x_scales), _ptr(w_mx), _ptr(out), n_tokens, hidden, inter), "spd_ffn_gate_up_mx")
+
     def set_kernel_timing(self, on: bool) -> None:
         _check(lib.spd_set_kernel_timing(self.h, int(on)), "spd_set_kernel_timing")
 
@@ -382,6 +404,12 @@ def pool_bytes(kind: int, page_tokens: int, n_kv_heads: int, dim_k: int, dim_v: 
     desc = spd_pool_desc(kind, page_tokens, n_kv_heads, dim_k, dim_v, num_pages)
     out = C.c_uint64()
     _check(lib.spd_pool_bytes(C.byref(desc), C.byref(out)), "spd_pool_bytes")
+    return out.value
+
+
+def ffn_mx_bytes(hidden: int, inter: int) -> int:
+    out = C.c_uint64()
+    _check(lib.spd_ffn_mx_bytes(hidden, inter, C.byref(out)), "spd_ffn_mx_bytes")
     return out.value
 
 
