@@ -50,7 +50,7 @@ enum {
 
 enum { SPD_PHASE_PREFILL = 0, SPD_PHASE_DECODE = 1 };
 
-typedef enum { SPD_KV_GQA = 0, SPD_KV_MLA_LATENT = 1, SPD_KV_MLA_LATENT_FP8 = 2 } spd_kv_kind;
+typedef enum { SPD_KV_GQA = 0, SPD_KV_MLA_LATENT = 1, SPD_KV_MLA_LATENT_FP8 = 2, SPD_KV_GQA_FP8 = 3 } spd_kv_kind;
 
 /* ------------------------------------------------------------------ context */
 
@@ -88,6 +88,17 @@ int spd_device_info(spd_ctx* ctx, int* total_cus, int* xcds, int* cu_granularity
  * attends over decode(code) * scale as it is, without that rounding (closer to the cached values than
  * the gathered rows, by less than bf16 resolves).  RoPE inside the decode step is not offered on such a
  * pool (SPD_EINVAL).
+ * GQA, 8 bits (the FP8 precision again; the format is this library's reading): the geometry of a GQA pool, but a cached row keeps OCP FP8 E4M3
+ * codes, with one power-of-two scale for the keys and one for the values of each block: 16 consecutive positions (from a multiple of 16 on)
+ * of one KV head.  The scale is the smallest 2^e, e >= -126, with which the block's largest finite magnitude does not pass 448, a code
+ * is x / 2^e rounded to nearest even (infinities and NaN: NaN): 2 dim + 1/4 bytes per token and head instead of 4 dim.  Every call takes and
+ * returns the same bf16 tensors as for a bf16 GQA pool.  spd_kv_gather hands back code * 2^e, which is exact in bf16, and the decode step attends
+ * over those values.  Rows are written front to back: a write (spd_kv_write, a step's rows, an appended token) that begins at a
+ * block's first position begins that block anew; one that begins further on keeps the block's rows ahead of it, under the larger of the block's
+ * scale and the one that the new rows need (where it grows, rows ahead are rounded again); rows of the block behind the written ones are no
+ * longer there.  A prefill step attends to its own rows as they are given (as on every pool) and to a cached prefix as it was cached before the
+ * step; with a prefix it brings all those rows together in library memory, 4 dim bytes per token and head, which the context keeps: SPD_ESTATE, and
+ * nothing changes, where that memory cannot be had or the phase's stream is being captured into a graph.
  * The byte layout inside a page is private to the library (it is arranged for the
  * decode kernel's matrix-core operand order); read or write pages only through
  * spd_kv_write / spd_kv_gather / the steps. */
@@ -191,7 +202,7 @@ int spd_shm_kv_free_list(spd_shm_pool* pool, int32_t* out, int64_t cap, int64_t*
  * of the scores is taken before scaling).
  *
  * Chunked prefill (paper, Evaluation "Baselines": the chunked-prefill variants): with
- * prefix_lens non-NULL (GQA pools only) request r already has prefix_lens[r] >= 0 tokens in its
+ * prefix_lens non-NULL (GQA pools, bf16 or 8 bits) request r already has prefix_lens[r] >= 0 tokens in its
  * pages and the rows given are the next piece of its prompt, at positions prefix .. prefix+len-1:
  *     out[i, h, :] = sum_{j <= prefix + i} softmax_j(scale * q[i, h, :] . K_r[j, g, :]) * V_r[j, g, :]
  * where K_r, V_r are the cached rows followed by the piece's own.  The step reserves blocks for

@@ -30,6 +30,12 @@ namespace spd {
 //       contiguous and holds the A operands (row = d, 4 consecutive tokens per lane) of two
 //       v_mfma_f32_16x16x16_bf16 for the value blocks 2*blk2 and 2*blk2 + 1.
 //
+// A GQA page in 8 bits has the same regions with one byte per entry, and behind them the scales: for each KV head and tile two bytes, of the
+// keys and of the values (mx.h).  A lane's 16-byte load of a tile's piece p (64 entries of the head each) is then
+//   K part: [p][quarter c][token t][16]: entries 64 p + 8 c .. + 7 and 64 p + 32 + 8 c .. + 7, the A operands of k-steps 2 p and 2 p + 1;
+//   V part: [p][token quad c][m][16]: entries 64 p + 16 i + m (i = byte / 4) of tokens 4 c + byte % 4.
+// Scales lie apart so that every load of a tile is 1 KiB of whole cache lines.  (They are read once per 64 tiles of a wave.)
+//
 // An MLA latent page keeps the natural order: P rows of 576 dims.  Its decode kernel stages rows
 // through LDS and reads them back in both operand orders (kernels_decode_mla.hip).
 // ---------------------------------------------------------------------------------------------
@@ -42,7 +48,10 @@ struct PoolGeom {
   int tiles_per_page;
   uint32_t tile_k_bytes, tile_v_bytes, tile_bytes, head_bytes;
   uint64_t page_bytes;
+  uint64_t scale_off;      // GQA in 8 bits: where a page's scales begin
 };
+// pools of K and V rows per KV head (bf16, or in 8 bits); the others hold latent rows
+__host__ __device__ inline bool gqa_kind(int kind) { return kind == SPD_KV_GQA || kind == SPD_KV_GQA_FP8; }
 
 __host__ __device__ inline uint32_t k_elem_offset(int t16, int d) { return ((d >> 3) * 16 + t16) * 8 + (d & 7); }
 __host__ __device__ inline uint32_t v_elem_offset(int t16, int d) {
@@ -53,11 +62,13 @@ inline PoolGeom make_geom(const spd_pool_desc& d) {
   PoolGeom g{};
   g.kind = d.kind; g.P = d.page_tokens; g.Hkv = d.n_kv_heads; g.dk = d.dim_k; g.dv = d.dim_v;
   g.tiles_per_page = d.page_tokens / TILE_T;
-  g.tile_k_bytes = d.kind == SPD_KV_MLA_LATENT_FP8 ? TILE_T * FP8_ROW_BYTES : TILE_T * d.dim_k * 2;
-  g.tile_v_bytes = d.kind == SPD_KV_GQA ? TILE_T * d.dim_v * 2 : 0;
+  const int width = d.kind == SPD_KV_GQA_FP8 ? 1 : 2;
+  g.tile_k_bytes = d.kind == SPD_KV_MLA_LATENT_FP8 ? TILE_T * FP8_ROW_BYTES : TILE_T * d.dim_k * width;
+  g.tile_v_bytes = gqa_kind(d.kind) ? TILE_T * d.dim_v * width : 0;
   g.tile_bytes = g.tile_k_bytes + g.tile_v_bytes;
   g.head_bytes = g.tiles_per_page * g.tile_bytes;
-  g.page_bytes = (uint64_t)g.head_bytes * d.n_kv_heads;
+  g.page_bytes = g.scale_off = (uint64_t)g.head_bytes * d.n_kv_heads;
+  if (d.kind == SPD_KV_GQA_FP8) g.page_bytes += ((uint64_t)2 * g.tiles_per_page * d.n_kv_heads + 127) & ~(uint64_t)127;
   return g;
 }
 
@@ -363,11 +374,18 @@ hipError_t launch_kv_write_fp8(const PoolGeom& g, char* pool_base, const TileDes
                                uint64_t copy_bytes = 0);
 hipError_t launch_kv_gather_fp8(const PoolGeom& g, const char* pool_base, const TileDesc* d_tiles, int n_tiles, void* out,
                                 const StepMark& mark, hipStream_t stream);
+// GQA pools in 8 bits (kernels_kv_gqa_fp8.hip): everything that KvRows says but the query rows; launch_kv_rows and launch_kv_gather lead there.
+// A block that d_tiles writes from its middle on must not be among d_cached: with k_all its earlier rows go there too, ahead of TileDesc.pad[1].
+hipError_t launch_kv_rows_gqa_fp8(const PoolGeom& g, char* pool_base, const TileDesc* d_tiles, int n_tiles, const void* k, const void* v,
+                                  const KvRows& x, const StepMark& mark, hipStream_t stream);
 hipError_t launch_meta_copy(void* dst, const void* src, uint64_t bytes, const StepMark& mark, hipStream_t stream);
 // What `d` rotates and appends, ahead of the attention launch: its queries are rotated to q_rot (with d.rot), the new tokens go into
 // their pages (with d.k_new).  d.items: n_items records in device memory.
 hipError_t launch_decode_prepare(const PoolGeom& g, char* pool_base, const DecodeLaunch& d, int n_items, void* q_rot, hipStream_t stream);
 hipError_t launch_decode_gqa(const PoolGeom& g, char* pool_base, const DecodeLaunch& d, hipStream_t stream);
+// pages in 8 bits (kernels_decode_fp8.hip); the two above lead there
+hipError_t launch_decode_prepare_fp8(const PoolGeom& g, char* pool_base, const DecodeLaunch& d, int n_items, void* q_rot, hipStream_t stream);
+hipError_t launch_decode_gqa_fp8(const PoolGeom& g, char* pool_base, const DecodeLaunch& d, hipStream_t stream);
 hipError_t launch_decode_mla(const PoolGeom& g, char* pool_base, const DecodeLaunch& d, hipStream_t stream);
 // The latent decode's workgroup fetches a record one word per thread and keeps it in LDS: as many pages as that leaves a chunk
 // may touch, and no record may be longer (checked again at the launch).

@@ -17,48 +17,18 @@
 //   O^T[dim, query] += V_tile^T[16 x 16] . P^T[16 x 16]  v_mfma_f32_16x16x16_bf16, d/16 blocks
 // Long contexts are split into chunks (split-K); partial (max, sum, O) triples go to a
 // workspace and are merged by the launch itself or by a small second kernel (split_merge.h).
+#include "decode_gqa.h"
 #include "internal.h"
 #include "rope_device.h"
 #include "split_merge.h"
 
 namespace spd {
 
-typedef unsigned short bf16_t;
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
-// two floats -> two bf16 (round to nearest even), packed low / high
-__device__ inline uint32_t pack_bf16_rne(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
-}
-
 template <int D>
 struct TileFrag {          // two 16-token tiles, K and V parts, in operand order
   uint4 k[2][D / 32];
   uint4 v[2][D / 32];
 };
-
-// A 16-byte load of data that is read exactly once (KV pages in a decode step): marked non-temporal,
-// so that the stream does not push the prefill partition's K/V tiles, which ARE re-read, out of the L2
-// the two partitions share.
-__device__ inline uint4 load_once(const uint4* p) {
-  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-  const u32x4 r = __builtin_nontemporal_load((const u32x4*)p);
-  return uint4{r.x, r.y, r.z, r.w};
-}
-
-// LDS written above by lanes of this wave is read below by other lanes of it (a wave's LDS accesses are served in order)
-__device__ inline void lds_visible_in_wave() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
-// Page ids of the tiles one wave streams, in its lanes: lane 2 i + u holds where tile u of the wave's i-th step lies.
-struct TileWindow { uint32_t lo, hi; };
 
 template <int D>
 __device__ inline void load_step(TileFrag<D>& f, const char* __restrict__ base, const TileWindow& w, int i, int lane) {
@@ -169,24 +139,7 @@ __device__ inline void compute_step(const TileFrag<D>& f, const bf16x8 (&qf)[D /
 // to the context with that token included.  As launches of their own the append and the rotation cost 5.6 us per step,
 // and more than the attention itself in a batch of a few short contexts.  Where a compute unit has many workgroups
 // they pay for that in turn, and decode_prepare_kernel does it for all of them.
-struct GqaArgs {
-  char* pool;
-  uint64_t page_bytes;
-  uint32_t head_bytes, tile_bytes;
-  int tiles_per_page;
-  const bf16_t *q, *k_new, *v_new;
-  bf16_t* out;
-  const char* items;
-  int item_stride, Hkv, H, G;
-  float c;                      // scale * log2(e)
-  int max_chunks;
-  const double* w;
-  int rot, off, interleaved;
-  float *ws_o, *ws_ml;
-  int32_t* put_chunks;
-  uint32_t* counters;
-  StepMark mark;
-};
+// (what it is given: decode_gqa.h)
 
 // grid (n_items * n_kv_heads), block 256; workgroup i serves KV head i % n_kv_heads of work item
 // i / n_kv_heads.  Heads vary fastest so that the round-robin placement of
@@ -461,20 +414,6 @@ __global__ __launch_bounds__(256) void decode_prepare_kernel(GqaArgs a, bf16_t* 
   }
 }
 
-static GqaArgs gqa_args(const PoolGeom& g, char* pool_base, const DecodeLaunch& d) {
-  GqaArgs a;
-  a.pool = pool_base;
-  a.page_bytes = g.page_bytes; a.head_bytes = g.head_bytes; a.tile_bytes = g.tile_bytes; a.tiles_per_page = g.tiles_per_page;
-  a.q = (const bf16_t*)d.q; a.k_new = (const bf16_t*)d.k_new; a.v_new = (const bf16_t*)d.v_new; a.out = (bf16_t*)d.out;
-  a.items = d.items; a.item_stride = d.item_stride;
-  a.Hkv = g.Hkv; a.H = d.H; a.G = d.H / g.Hkv;
-  a.c = d.scale * 1.4426950408889634f;
-  a.max_chunks = d.max_chunks;
-  a.w = d.w; a.rot = d.rot; a.off = d.off; a.interleaved = d.interleaved;
-  a.ws_o = d.ws_o; a.ws_ml = d.ws_ml; a.put_chunks = d.put_chunks; a.counters = d.counters; a.mark = d.mark;
-  return a;
-}
-
 template <int D>
 static hipError_t launch_decode_gqa_t(const PoolGeom& g, char* pool_base, const DecodeLaunch& d, hipStream_t stream) {
   const dim3 grid((unsigned)d.n_wgs * g.Hkv);
@@ -486,12 +425,14 @@ static hipError_t launch_decode_gqa_t(const PoolGeom& g, char* pool_base, const 
 }
 
 hipError_t launch_decode_gqa(const PoolGeom& g, char* pool_base, const DecodeLaunch& d, hipStream_t stream) {
+  if (g.kind == SPD_KV_GQA_FP8) return launch_decode_gqa_fp8(g, pool_base, d, stream);
   if (g.dk == 128) return launch_decode_gqa_t<128>(g, pool_base, d, stream);
   if (g.dk == 64) return launch_decode_gqa_t<64>(g, pool_base, d, stream);
   return hipErrorInvalidValue;
 }
 
 hipError_t launch_decode_prepare(const PoolGeom& g, char* pool_base, const DecodeLaunch& d, int n_items, void* q_rot, hipStream_t stream) {
+  if (g.kind == SPD_KV_GQA_FP8) return launch_decode_prepare_fp8(g, pool_base, d, n_items, q_rot, stream);
   const GqaArgs a = gqa_args(g, pool_base, d);
   if (g.dk == 128) hipLaunchKernelGGL(decode_prepare_kernel<128>, dim3((unsigned)n_items), dim3(256), 0, stream, a, (bf16_t*)q_rot);
   else if (g.dk == 64) hipLaunchKernelGGL(decode_prepare_kernel<64>, dim3((unsigned)n_items), dim3(256), 0, stream, a, (bf16_t*)q_rot);

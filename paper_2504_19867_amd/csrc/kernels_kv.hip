@@ -591,7 +591,10 @@ hipError_t launch_meta_copy(void* dst, const void* src, uint64_t bytes, const St
   return hipGetLastError();
 }
 
-bool kv_rows_supported(const PoolGeom& g) { return g.kind == SPD_KV_GQA && g.dk <= 128 && g.dv <= 128 && g.Hkv >= 2; }
+bool kv_rows_supported(const PoolGeom& g) {
+  if (g.kind == SPD_KV_GQA_FP8) return true;
+  return g.kind == SPD_KV_GQA && g.dk <= 128 && g.dv <= 128 && g.Hkv >= 2;
+}
 
 // KV heads per workgroup.  A workgroup takes its heads one after the other, in code that it runs once, so where there are compute units to
 // spare each head more in it is time: 0.9 us with rotation, 0.6 without.  Where there are not, more workgroups mean more reads of the
@@ -607,6 +610,7 @@ static int heads_per_workgroup(int n_tiles, int Hkv, int cus, bool rope) {
 
 hipError_t launch_kv_rows(const PoolGeom& g, char* pool_base, const TileDesc* d_tiles, int n_tiles, const void* k, const void* v,
                           const KvRows& x, const StepMark& mark, hipStream_t stream) {
+  if (g.kind == SPD_KV_GQA_FP8) return launch_kv_rows_gqa_fp8(g, pool_base, d_tiles, n_tiles, k, v, x, mark, stream);
   const int HG = heads_per_workgroup(n_tiles + x.n_cached, g.Hkv, x.cus, x.rope_w != nullptr);
   RowsArgs a{};
   a.base = pool_base;
@@ -652,6 +656,12 @@ hipError_t launch_kv_write(const PoolGeom& g, char* pool_base, const TileDesc* d
 hipError_t launch_kv_gather(const PoolGeom& g, const char* pool_base, const TileDesc* d_tiles, int n_tiles, void* k_out,
                             void* v_out, const StepMark& mark, hipStream_t stream) {
   if (n_tiles <= 0) return hipSuccess;
+  if (g.kind == SPD_KV_GQA_FP8) {
+    KvRows x;
+    x.d_cached = d_tiles; x.n_cached = n_tiles;
+    x.k_all = k_out; x.v_all = v_out;
+    return launch_kv_rows_gqa_fp8(g, (char*)pool_base, nullptr, 0, nullptr, nullptr, x, mark, stream);
+  }
   hipLaunchKernelGGL(kv_gather_kernel, dim3(n_tiles, g.Hkv), dim3(256), 0, stream, pool_base, g.page_bytes,
                      g.head_bytes, g.tile_bytes, g.tile_k_bytes, d_tiles, (bf16_t*)k_out, (bf16_t*)v_out, g.Hkv, g.dk,
                      g.dv, g.kind == SPD_KV_MLA_LATENT ? 1 : 0, mark);

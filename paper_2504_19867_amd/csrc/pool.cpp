@@ -15,7 +15,7 @@ thread_local int g_last_hip_error = 0;
 static bool desc_ok(const spd_pool_desc* d) {
   if (!d || d->num_pages <= 0 || d->num_pages > INT32_MAX) return false;
   if (d->page_tokens <= 0 || d->page_tokens % TILE_T != 0 || d->page_tokens > 1024) return false;
-  if (d->kind == SPD_KV_GQA) {
+  if (gqa_kind(d->kind)) {
     if (d->n_kv_heads <= 0 || d->n_kv_heads > 1024) return false;
     if (d->dim_k != d->dim_v) return false;
     return d->dim_k == 64 || d->dim_k == 128;

@@ -80,7 +80,7 @@ static int kv_copy(spd_ctx* ctx, spd_pool* pool, int phase, uint64_t req_id, int
   if (!ctx || !pool || pool->ctx != ctx || phase < 0 || phase > 1 || start_pos < 0 || n_tokens <= 0 || !k)
     return SPD_EINVAL;
   const PoolGeom& g = pool->geom;
-  if ((g.kind == SPD_KV_GQA) != (v != nullptr)) return SPD_EINVAL;
+  if (gqa_kind(g.kind) != (v != nullptr)) return SPD_EINVAL;
   if (misaligned16(k, v)) return SPD_EINVAL;
   if (ctx->device < 0) return SPD_ESTATE;
   // the request's table, if it holds the positions named (caller holds pool->mu)
@@ -144,7 +144,7 @@ extern "C" int spd_prefill_step(spd_ctx* ctx, spd_pool* pool, const spd_prefill_
   const PoolGeom& g = pool->geom;
   if (b->n_q_heads % b->n_kv_heads != 0 || b->cu_seqlens[0] != 0) return SPD_EINVAL;
   if (!(b->scale > 0.f) || !std::isfinite(b->scale)) return SPD_EINVAL;
-  if (g.kind == SPD_KV_GQA) {
+  if (gqa_kind(g.kind)) {
     if (b->latent || b->n_kv_heads != g.Hkv || b->dim_qk != g.dk || b->dim_v != g.dv) return SPD_EINVAL;
   } else {
     if (!b->latent || b->n_kv_heads != b->n_q_heads) return SPD_EINVAL;
@@ -152,7 +152,7 @@ extern "C" int spd_prefill_step(spd_ctx* ctx, spd_pool* pool, const spd_prefill_
   if (!prefill_shape_supported(b->dim_qk, b->dim_v)) return SPD_EINVAL;
   if (misaligned16(b->q, b->k, b->v, b->out, b->latent)) return SPD_EINVAL;
   if (b->rope) {
-    if (g.kind != SPD_KV_GQA) return SPD_EINVAL;
+    if (!gqa_kind(g.kind)) return SPD_EINVAL;
     int rrc = rope_config_check(b->rope);
     if (rrc != SPD_OK) return rrc;
     if (b->rope->rotary_dim % 16 || b->rope->rotary_offset % 8 || b->rope->rotary_offset + b->rope->rotary_dim > b->dim_qk)
@@ -167,7 +167,7 @@ extern "C" int spd_prefill_step(spd_ctx* ctx, spd_pool* pool, const spd_prefill_
   // chunked prefill: some request continues a prompt whose first prefix_lens[r] tokens are cached
   bool chunked = false;
   if (b->prefix_lens) {
-    if (g.kind != SPD_KV_GQA) return SPD_EINVAL;
+    if (!gqa_kind(g.kind)) return SPD_EINVAL;
     for (int r = 0; r < b->n_req; ++r) {
       if (b->prefix_lens[r] < 0) return SPD_EINVAL;
       chunked = chunked || b->prefix_lens[r] > 0;
@@ -189,12 +189,15 @@ extern "C" int spd_prefill_step(spd_ctx* ctx, spd_pool* pool, const spd_prefill_
   if (ctx->env_prefill_persistent >= 0) persistent = ctx->env_prefill_persistent != 0;   // experiment switch
   // Chunked: the attention kernel's keys and values as dense rows, brought together for it where that pays and there is memory for them
   // (K whole pages of 4 KiB: the kernel loads rows in 1 KiB pieces, which should not straddle cache lines) ...
+  // Pages in 8 bits are read by no prefill kernel: their rows are always brought together, or the step is refused.
+  const bool eight = g.kind == SPD_KV_GQA_FP8;
   char *rows_k = nullptr, *rows_v = nullptr;
   const size_t k_bytes = align4k((size_t)n_keys * g.Hkv * g.dk * 2), v_bytes = (size_t)n_keys * g.Hkv * g.dv * 2;
-  if (chunked && k_bytes + v_bytes <= MOST_DENSE_BYTES &&
-      dense_rows_pay(b->cu_seqlens, b->prefix_lens, b->n_req, b->n_q_heads, b->n_kv_heads, g.dk, share, b->rope != nullptr)) {
+  if (chunked && (eight || (k_bytes + v_bytes <= MOST_DENSE_BYTES &&
+                            dense_rows_pay(b->cu_seqlens, b->prefix_lens, b->n_req, b->n_q_heads, b->n_kv_heads, g.dk, share, b->rope != nullptr)))) {
     rows_k = rows_reserve(ctx, k_bytes + v_bytes);
     if (rows_k) rows_v = rows_k + k_bytes;
+    else if (eight) return SPD_ESTATE;
   }
   // ... else out of the pages.  kv_cu: where each request's begin, its first dense row or its first unit of 16 tokens in the list that the
   // kernel finds them with
@@ -230,11 +233,13 @@ extern "C" int spd_prefill_step(spd_ctx* ctx, spd_pool* pool, const spd_prefill_
   // page write, RoPE and dense rows in one launch, where that kernel takes the pool's shape (elsewhere the rows, the new ones included, are
   // gathered out of the pages by a launch of its own)
   const bool one_launch = kv_rows_supported(g);
+  // (in 8 bits the page write changes the whole block that a piece begins in, and hands out its earlier rows itself)
+  auto cached_rows = [&](int32_t pre, int32_t len) -> int32_t { return !one_launch ? pre + len : eight ? pre - pre % TILE_T : pre; };
   size_t n_descs = 0, n_gather = 0;
   for (int r = 0; r < b->n_req; ++r) {
     const int32_t len = b->cu_seqlens[r + 1] - b->cu_seqlens[r], pre = chunked ? b->prefix_lens[r] : 0;
     n_descs += tile_desc_count(pre, len);
-    if (rows_k) n_gather += tile_desc_count(0, one_launch ? pre : pre + len);
+    if (rows_k) n_gather += tile_desc_count(0, cached_rows(pre, len));
   }
   size_t off_chain = align16(work.size() * sizeof(PrefillWork));
   size_t off_range = align16(off_chain + chain.size() * sizeof(int32_t));
@@ -247,7 +252,7 @@ extern "C" int spd_prefill_step(spd_ctx* ctx, spd_pool* pool, const spd_prefill_
   // queries 28 / 35 us on 128 CUs, 16 MiB 42 / 50, 32 MiB 65 / 70, 64 MiB 118 / 119, 128 MiB 239 / 230; on 96 CUs level at 64 MiB
   // too (147 / 144), 320 MiB 785 / 762.  On 256 CUs one launch stays 3 to 6 % ahead up to 320 MiB, which this line leaves.
   const int32_t n_rows = b->cu_seqlens[b->n_req];
-  const bool own_rope = b->rope && (!one_launch || (int64_t)n_rows * b->n_q_heads * b->dim_qk * 2 > Q_IN_ONE_LAUNCH);
+  const bool own_rope = b->rope && (!one_launch || eight || (int64_t)n_rows * b->n_q_heads * b->dim_qk * 2 > Q_IN_ONE_LAUNCH);
   size_t off_pos = align16(off_units + (paged ? (size_t)kv_cu.back() * sizeof(int32_t) : n_gather * sizeof(TileDesc)));
   size_t bytes = align16(off_pos + (own_rope ? sizeof(int32_t) * (size_t)n_rows : 0));
   const size_t off_w = bytes, w_bytes = b->rope ? sizeof(double) * (size_t)(b->rope->rotary_dim / 2) : 0;
@@ -278,7 +283,7 @@ extern "C" int spd_prefill_step(spd_ctx* ctx, spd_pool* pool, const spd_prefill_
       const int n_new = build_tile_descs(g, entry.data(), pre, len, row0, h_desc);
       if (rows_k) {
         for (int i = 0; i < n_new; ++i) h_desc[i].pad[1] = kv_cu[(size_t)r] + pre + (h_desc[i].src_row - row0);
-        h_gather += build_tile_descs(g, entry.data(), 0, one_launch ? pre : pre + len, kv_cu[(size_t)r], h_gather);
+        h_gather += build_tile_descs(g, entry.data(), 0, cached_rows(pre, len), kv_cu[(size_t)r], h_gather);
       }
       h_desc += n_new;
       if (paged) {
@@ -308,8 +313,8 @@ extern "C" int spd_prefill_step(spd_ctx* ctx, spd_pool* pool, const spd_prefill_
     }
     if ((rc = rope_table(step, b->rope, st->host + off_w, st->dev + off_w, &mark, &rope_w)) != SPD_OK) return rc;
   }
-  const void* page_src_k = g.kind == SPD_KV_GQA ? b->k : b->latent;
-  const void* page_src_v = g.kind == SPD_KV_GQA ? b->v : nullptr;
+  const void* page_src_k = gqa_kind(g.kind) ? b->k : b->latent;
+  const void* page_src_v = gqa_kind(g.kind) ? b->v : nullptr;
   // the page write reads its descriptors straight out of the pinned staging buffer, and extra workgroups of the
   // same kernel copy the whole staging buffer to its device twin, where the attention kernel finds its lists
   const spd_rope_config* rc_ = b->rope;
@@ -380,7 +385,7 @@ static int decode_step_impl(spd_ctx* ctx, spd_pool* pool, const spd_decode_batch
   if (b->n_q_heads % g.Hkv != 0 || b->n_q_heads / g.Hkv > 16) return SPD_EINVAL;
   if (!(b->scale > 0.f) || !std::isfinite(b->scale)) return SPD_EINVAL;
   const bool append = b->k_new != nullptr;
-  if (append && (g.kind == SPD_KV_GQA) != (b->v_new != nullptr)) return SPD_EINVAL;
+  if (append && gqa_kind(g.kind) != (b->v_new != nullptr)) return SPD_EINVAL;
   if (!append && b->v_new) return SPD_EINVAL;
   if (misaligned16(b->q, b->out, b->k_new, b->v_new)) return SPD_EINVAL;
   spd_phase_state& ds = ctx->phase[SPD_PHASE_DECODE];
@@ -398,7 +403,7 @@ static int decode_step_impl(spd_ctx* ctx, spd_pool* pool, const spd_decode_batch
   if (ctx->device < 0) return SPD_ESTATE;
 
   const int B = b->n_req;
-  const bool mla = g.kind != SPD_KV_GQA;
+  const bool mla = !gqa_kind(g.kind);
   const int units_per_page = g.P / TILE_T;
   int64_t sum_units = 0;
   int32_t max_units = 0, max_pages = 0;
@@ -444,7 +449,7 @@ static int decode_step_impl(spd_ctx* ctx, spd_pool* pool, const spd_decode_batch
   const bool many = !mla && gqa_many(n_wgs, share, g.dk);
   bool twin = many || (size_t)n_items * g.Hkv * stride > 131072;
   bool prepare = many && (append || b->rope) &&
-                 gqa_prepares(sum_units * TILE_T * g.Hkv * (g.dk + g.dv) * (int64_t)sizeof(uint16_t), n_wgs, share, b->rope != nullptr);
+                 gqa_prepares(sum_units * g.Hkv * (int64_t)g.tile_bytes, n_wgs, share, b->rope != nullptr);
   if (noalloc && bytes > NOALLOC_TWIN_BYTES) twin = prepare = false;
   // Split-K partials of a GQA launch of few workgroups are merged by that launch, where a request has few chunks; else by a
   // launch of its own.  Whole step over 128-dim heads, in the launch / on its own: 24 workgroups, 3 chunks 9.1 / 10.9 us; 192, 9
