@@ -22,6 +22,7 @@
 // (ffn_gate_up_stream_kernel); between 128 and 256 tokens there are 128 x 128 tiles (ffn_gate_up_small_kernel: four waves, two
 // workgroups per compute unit), where those are the faster ones (small_tiles_pay).
 #include "ffn_stream.h"
+#include "ffn_tiles.h"
 #include "internal.h"
 
 #include <type_traits>
@@ -41,35 +42,6 @@ constexpr int BK = 32;                          // hidden entries per slice
 __device__ inline uint32_t cvt_bf16(float a) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, a}, bf16x2)) & 0xffffu;
 }
-// 16 bytes per lane from global memory to LDS: lane i's data lands at lds_byte_addr + 16 * i.
-// The compiler does not see this write; completion is tracked by hand with vmcnt.
-__device__ inline void dma16s(const void* sbase, uint32_t voff, uint32_t lds_byte_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_byte_addr), "v"(voff), "s"(sbase) : "memory");
-}
-#define SPD_WAIT_VMCNT(N) __builtin_amdgcn_s_waitcnt(((N) & 15) | (7 << 4) | (15 << 8) | (((N) >> 4) << 14))
-
-// Which tile the workgroups of an XCD take, in the order in which they take them.  Workgroup b runs on XCD b % xcds, and the
-// workgroups of an XCD start in the order of b.  Every XCD takes a contiguous range of weight tiles (columns) and all token tiles;
-// inside it the tiles are ordered so that the 16 or so workgroups running together form a block of about 4 x 4 tiles:
-// each slice of x and of the weights that misses the XCD's L2 then feeds four workgroups.
-struct TileOrder {
-  int tiles_m, start, cnt;                        // this XCD's weight tiles: cnt from `start` on
-  __device__ TileOrder(int tiles_m_, int tiles_n, int xcds) : tiles_m(tiles_m_) {
-    const int xcd = (int)blockIdx.x % xcds, base = tiles_n / xcds, rem = tiles_n % xcds;
-    cnt = base + (xcd < rem ? 1 : 0);
-    start = xcd * base + min(xcd, rem);
-  }
-  __device__ int slots() const { return cnt * tiles_m; }
-  __device__ void tile(int slot, int& tm, int& tn) const {
-    const int full = cnt / 4;                     // column blocks of four weight tiles; the last one narrower
-    const bool in_full = slot < full * 4 * tiles_m;
-    const int cb = in_full ? slot / (4 * tiles_m) : full, wb = in_full ? 4 : cnt - 4 * full;
-    const int q = slot - cb * 4 * tiles_m;
-    tm = q / wb;
-    tn = start + 4 * cb + q % wb;
-  }
-};
-
 // 128 tokens x 128 joint columns, 2 x 2 waves with 64 tokens x 64 joint columns each, two workgroups per compute unit; a ring of
 // four stages with one s_barrier per slice, operands read a slice ahead of the MFMAs into a second set of registers.
 __global__ __launch_bounds__(256, 2) void ffn_gate_up_small_kernel(const bf16_t* __restrict__ x, const bf16_t* __restrict__ w,

@@ -6,9 +6,11 @@
 // scale byte of its 32 entries.  Weights are the A operand, so that a lane has consecutive outputs of one token.  Where the E2M1 lane of row r
 // and quarter c of a step of 128 entries holds the entries 32 c .. 32 c + 31, the E4M3 lane holds 16 c .. 16 c + 15 and 64 + 16 c ..
 // 64 + 16 c + 15: that is the order in which the instruction multiplies; the scales go by quarters in both.
+#include "ffn_tiles.h"
 #include "mx.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace spd {
 
@@ -29,6 +31,8 @@ __device__ inline float silu(float g) { return g * __builtin_amdgcn_rcpf(1.f + _
 __device__ inline i32x8 e2m1_operand(u32x4 a) { return i32x8{(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0}; }
 __device__ inline i32x8 e4m3_operand(u32x4 a, u32x4 b) { return i32x8{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w}; }
 constexpr int E4M3 = 0, E2M1 = 4;                  // the instructions' names of the formats
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef unsigned int u32x4_any __attribute__((ext_vector_type(4), aligned(2)));   // `out` is only promised to be aligned to its entries
 }  // namespace
 
 // ---- the packed weights.  A tile is 128 outputs x 128 hidden entries; unit u of it (16 outputs) keeps, from byte 2048 u on, the codes of its
@@ -148,9 +152,235 @@ __global__ __launch_bounds__(64) void ffn_gate_up_mx_kernel(const char* __restri
   o[0] = (bf16_t)y0; o[1] = (bf16_t)(y0 >> 16); o[2] = (bf16_t)y1; o[3] = (bf16_t)(y1 >> 16);
 }
 
+// 256 tokens x 128 outputs (256 rows of weights).  As ffn_gate_up_large_kernel: eight waves in two groups that run half a step apart, one group's
+// matrix instructions beside the other group's loads and operand reads, an s_barrier at every change; a workgroup walks the tiles slot, slot +
+// gridDim / xcds, .. with its loads running ahead across tiles.  A step is 64 hidden entries, 8 v_mfma_scale_f32_32x32x64 per wave, 512 cycles at the
+// rate of the 8-bit operand; both operands' bytes come in pairs of steps (128 entries: whole cache lines of x, a tile of the packed weights), three
+// pairs in LDS: 3 x (32 KiB x, 16 KiB codes of weights, 1 KiB of scales of either).
+__global__ __launch_bounds__(512, 2) void ffn_gate_up_mx_large_kernel(const char* __restrict__ x, const uint32_t* __restrict__ xs, const char* __restrict__ w,
+                                                                      bf16_t* __restrict__ out, int T, int K, int I, int tiles_m, int tiles_n, int xcds,
+                                                                      StepMark mark) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) store_mark(mark);
+  constexpr int BM = 256, X_PAIR = BM * 128, W_PAIR = SCALES_AT, S_PAIR = 2048, NP = 3;   // bytes of a pair, pairs in LDS
+  constexpr int W_LDS = NP * X_PAIR, S_LDS = W_LDS + NP * W_PAIR;
+  __shared__ __attribute__((aligned(1024))) char smem[S_LDS + NP * S_PAIR];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n32 = lane & 31, hh = lane >> 5;
+  const int wm = wave >> 2, wn = wave & 3;        // wm: also the wave's group
+  const TileOrder order(tiles_m, tiles_n, xcds);
+  const int n_slots = order.slots(), slot_step = (int)gridDim.x / xcds;
+  int slot = (int)blockIdx.x / xcds;
+  if (slot >= n_slots) return;
+  const uint32_t smem_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+  const int n_pairs = K / 128, n_steps = 2 * n_pairs;
+  int left = ((n_slots - 1 - slot) / slot_step + 1) * n_steps;   // steps of all tiles of this workgroup from the current one on
+
+  // ---- loads, in two halves of a pair: 128 rows of x (two instructions per wave; slot s of a row of 128 bytes holds the row's chunk
+  // s ^ ((row >> 1) & 7)) and four units of the weights (one); with the first half the scales (one: waves 0 .. 3 the tokens', 4 .. 7 the weights').
+  // Token rows past T re-read row T - 1.
+  const int x_chunk = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7);
+  uint32_t x_voff[2][2], s_voff;                  // [half][j]
+  const uint32_t w_voff = (uint32_t)lane * 16;
+  const char *x_ptr, *w_ptr, *s_ptr;              // the next pair's
+  size_t s_step;                                  // of s_ptr, from pair to pair
+  int l_slot = slot, l_left = n_pairs;            // its tile, and pairs until that tile's end
+  auto l_tile = [&]() __attribute__((always_inline)) {
+    int tm, tn;
+    order.tile(l_slot, tm, tn);
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        x_voff[hf][j] = (uint32_t)min(128 * hf + 8 * (wave + 8 * j) + (lane >> 3), T - 1 - tm * BM) * (uint32_t)K + (uint32_t)x_chunk * 16;
+    x_ptr = x + (size_t)(tm * BM) * K;
+    w_ptr = w + (size_t)tn * n_pairs * FFN_MX_TILE_BYTES + wave * 1024;
+    if (wave < 4) {
+      s_ptr = (const char*)(xs + tm * BM);
+      s_step = (size_t)T * 4;
+      s_voff = (uint32_t)min(64 * wave + lane, T - 1 - tm * BM) * 4;
+    } else {
+      s_ptr = w + (size_t)tn * n_pairs * FFN_MX_TILE_BYTES + SCALES_AT;
+      s_step = FFN_MX_TILE_BYTES;
+      s_voff = (uint32_t)(64 * (wave - 4) + lane) * 4;
+    }
+  };
+  l_tile();
+  auto load = [&](int stage, int hf) __attribute__((always_inline)) {
+    const uint32_t lds = smem_base + stage * X_PAIR + hf * (X_PAIR / 2) + wave * 1024;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) dma16s(x_ptr, x_voff[hf][j], lds + j * 8192);
+    dma16s(w_ptr + hf * 8192, w_voff, smem_base + W_LDS + stage * W_PAIR + hf * 8192 + wave * 1024);
+    if (hf == 0) {
+      dma4s(s_ptr, s_voff, smem_base + S_LDS + stage * S_PAIR + wave * 256);
+    } else {
+      x_ptr += 128;
+      w_ptr += FFN_MX_TILE_BYTES;
+      s_ptr += s_step;
+      if (--l_left == 0) {
+        l_left = n_pairs;
+        l_slot += slot_step;
+        if (l_slot < n_slots) l_tile();
+      }
+    }
+  };
+
+  // ---- LDS operand addresses.  Of a step's 64 entries the lane half hh has, of the weights, the quarter 2 sl + hh (32 entries, 16 bytes); of x the
+  // chunks 4 sl + hh and 4 sl + 2 + hh; and of both the scale of that quarter.  The stage is part of a read's 16-bit immediate; the third
+  // pair of x lies beyond its reach and gets lane addresses of its own.
+  int x_off[2][2][2];                             // [third stage][step of the pair][chunk]
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int sl = 0; sl < 2; ++sl) {
+      x_off[0][sl][j] = (wm * 128 + n32) * 128 + ((4 * sl + 2 * j + hh) ^ ((n32 >> 1) & 7)) * 16;
+      x_off[1][sl][j] = x_off[0][sl][j] + 2 * X_PAIR;
+      asm volatile("" : "+v"(x_off[1][sl][j]));   // a value of its own, not "x_off + constant" to be recomputed
+    }
+  const int unit = 2 * wn + (n32 >> 4), row = n32 & 15;
+  int w_off = W_LDS + unit * 2048 + hh * 256 + row * 16, ws_off = S_LDS + 1024 + unit * 128 + row * 8, xs_off = S_LDS + (wm * 128 + n32) * 4;
+  asm volatile("" : "+v"(w_off), "+v"(ws_off), "+v"(xs_off));
+  u32x4 ox[4][2], ow[2];
+  uint32_t sx[4], sw[2];                          // scale bytes: of the pair's first step in byte 0, of its second in byte 2
+  // acc[mb][0] = gate, acc[mb][1] = up: element i of lane (n32, hh) is output 8 (i / 4) + 4 hh + i % 4 of token 32 mb + n32
+  f32x16 acc[4][2];
+  auto clear = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[mb][nb][e] = 0.f;
+  };
+  clear();
+  auto barrier = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // ahead of the first step: pairs 0 and 1, as the steps -4 .. -1 would load them
+  load(0, 0);
+  load(0, 1);
+  if (left > 2) {
+    load(1, 0);
+    load(1, 1);
+    SPD_WAIT_VMCNT(7);
+  } else {
+    SPD_WAIT_VMCNT(0);
+  }
+  barrier();                                      // pair 0 is there
+  if (wm) barrier();                              // the second group starts half a step later
+
+  int ct = 0;                                     // step of the tile
+  int ready = 0;                                  // steps that need not wait: the end of a tile has awaited all loads up to it
+  auto step = [&](auto stc) __attribute__((always_inline)) {
+    constexpr int ST = stc, SL = ST & 1, P = ST / 2;   // step modulo the ring's period; step of the pair
+    // Loading and reading half of step u, of pair p.  The stage being loaded held pair p - 1, whose reads both groups had behind them at the
+    // last barrier.  At this half's end the wave's own reads are done, and so is what it loaded up to step u - 2: its part of the pair that
+    // the other group may read a whole step from now, this one in one and a half.
+    if (left > 4) load((P + 2) % NP, SL);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (SL == 0) {
+      const uint2 two = *(const uint2*)(smem + ws_off + P * S_PAIR);
+      sw[0] = two.x; sw[1] = two.y;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sx[r] = *(const uint32_t*)(smem + xs_off + P * S_PAIR + r * 128);
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) ow[r] = *(const u32x4*)(smem + w_off + P * W_PAIR + SL * 512 + r * 1024);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) ox[r][j] = *(const u32x4*)(smem + x_off[P == 2][SL][j] + (P == 1 ? X_PAIR : 0) + r * (32 * 128));
+    __builtin_amdgcn_sched_barrier(0);
+    if (ready > 0) --ready;
+    else if (left >= 5) SPD_WAIT_VMCNT(7);        // this step's loads and those of the one before: three and four
+    else if (left == 4) SPD_WAIT_VMCNT(3);
+    else SPD_WAIT_VMCNT(0);
+    __builtin_amdgcn_s_waitcnt(0xc07f);           // lgkmcnt(0)
+    if constexpr (SL == 0) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) sw[r] >>= 8 * hh;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sx[r] >>= 8 * hh;
+    }
+    barrier();
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb)
+        acc[mb][nb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(e2m1_operand(ow[nb]), e4m3_operand(ox[mb][0], ox[mb][1]), acc[mb][nb], E2M1, E4M3,
+                                                                      2 * SL, (int)sw[nb], 2 * SL, (int)sx[mb]);
+    // (the products belong here: without side effects of their own they would be moved past the barriers to where their sums are used)
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb) asm volatile("" : "+v"(acc[mb][0]), "+v"(acc[mb][1]));
+    __builtin_amdgcn_s_setprio(0);
+    barrier();
+    --left;
+    ++ct;
+  };
+  // ---- the tile's end, as in ffn_gate_up_large_kernel: the halves of the wave exchange four outputs each, so that a lane stores eight consecutive
+  // ones.  All loads so far are awaited ahead of the first store: the next two steps then have nothing to wait for, and do not wait for the
+  // stores either.
+  auto finish_tile = [&]() __attribute__((always_inline)) {
+    int tm, tn;
+    order.tile(slot, tm, tn);
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb) {
+      uint32_t y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        y[i] = pack_bf16(silu(acc[mb][0][2 * i]) * acc[mb][1][2 * i], silu(acc[mb][0][2 * i + 1]) * acc[mb][1][2 * i + 1]);
+      if (mb == 0) SPD_WAIT_VMCNT(0);
+      const int t = tm * BM + wm * 128 + mb * 32 + n32;
+      bf16_t* o = out + (size_t)t * I + tn * 128 + wn * 32 + 8 * hh;
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        // (machine code: the compiler's builtin for the swap loses the second result)
+        asm volatile("s_nop 1\n\tv_permlane32_swap_b32 %0, %1\n\tv_permlane32_swap_b32 %2, %3\n\ts_nop 1"
+                     : "+v"(y[4 * p]), "+v"(y[4 * p + 2]), "+v"(y[4 * p + 1]), "+v"(y[4 * p + 3]));
+        if (t < T) *(u32x4_any*)(o + 16 * p) = u32x4_any{y[4 * p], y[4 * p + 1], y[4 * p + 2], y[4 * p + 3]};
+      }
+    }
+  };
+  // a pair of steps and, behind a tile's last one, its end; false behind the last tile
+  auto pair = [&](auto pc) __attribute__((always_inline)) -> bool {
+    constexpr int P = pc;
+    step(std::integral_constant<int, 2 * P>{});
+    step(std::integral_constant<int, 2 * P + 1>{});
+    if (ct == n_steps) {
+      finish_tile();
+      if (left == 0) return false;
+      slot += slot_step;
+      clear();
+      ct = 0;
+      ready = 2;
+    }
+    return true;
+  };
+  for (;;) {
+    if (!pair(std::integral_constant<int, 0>{})) break;
+    if (!pair(std::integral_constant<int, 1>{})) break;
+    if (!pair(std::integral_constant<int, 2>{})) break;
+  }
+  if (!wm) barrier();                             // as many as the second group
+}
+
 hipError_t launch_ffn_gate_up_mx(const void* x, const void* x_scales, const void* w_mx, void* out, int T, int K, int I, int xcds, int cus, bool exclusive,
                                  const StepMark& mark, hipStream_t stream) {
-  (void)xcds; (void)cus; (void)exclusive;
+  if (T > 128) {
+    const int tiles_m = (int)(((int64_t)T + 255) / 256), tiles_n = I / 128;
+    const int persistent = exclusive ? cus : 0;    // workgroups, one per compute unit of a share that has them to itself; 0: one per tile
+    if (tiles_n < xcds || persistent % xcds) xcds = 1;
+    int64_t n = xcds > 1 ? (int64_t)((tiles_n + xcds - 1) / xcds) * tiles_m * xcds : (int64_t)tiles_m * tiles_n;
+    if (n > INT32_MAX) return hipErrorInvalidValue;
+    if (persistent) n = std::min<int64_t>(n, persistent);
+    hipLaunchKernelGGL(ffn_gate_up_mx_large_kernel, dim3((unsigned)n), dim3(512), 0, stream, (const char*)x, (const uint32_t*)x_scales, (const char*)w_mx,
+                       (bf16_t*)out, T, K, I, tiles_m, tiles_n, xcds, mark);
+    return hipGetLastError();
+  }
   const int64_t wgs = (int64_t)(I / 16) * ((T + (int64_t)15) / 16);
   if (wgs > INT32_MAX) return hipErrorInvalidValue;
   hipLaunchKernelGGL(ffn_gate_up_mx_kernel, dim3((unsigned)wgs), dim3(64), 0, stream, (const char*)x, (const uint32_t*)x_scales, (const char*)w_mx,
