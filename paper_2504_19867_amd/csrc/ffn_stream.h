@@ -32,4 +32,23 @@ inline int ffn_stream_units(int blocks, int units, int K, int cus) {
   return per_wg;
 }
 
+// The same for weights in MXFP4 (ffn_gate_up_mx_stream_kernel).  Eight to four units: a wave each; three or two (from 65 tokens on four or two): two
+// waves halve a unit's slices.  One workgroup's time by units, all workgroups at once (hidden 8192, inter 7168 on 256 CUs), 1 token, eight to two units:
+// 22.8, 21.3, 18.8, 16.3, 14.8, 12.0, 10.1 us; 64 tokens 29.8, 27.6, 26.5, 26.6, 21.3, 18.8, 16.9; 128 tokens, eight, four, two: 46.8, 30.8, 30.  Inter
+// 14336 of hidden 4096 (896 units), 1 token, eight units / the ones taken: 64 CUs 23 / 21.6 us (7), 128 13.2 / 12.4 (7), 256 13.2 / 9.8 (4).
+inline int ffn_mx_stream_units(int blocks, int units, int cus) {
+  const int cost[] = {blocks <= 4 ? 47 : 61, 57, blocks <= 4 ? 67 : 68, 76, 85, 94, 100};   // of a workgroup of 2 .. 8 units
+  int per_wg = 8;
+  long least = 0;
+  for (int n = 8; n >= 2; --n) {
+    if (blocks > 4 && n != 8 && n != 4 && n != 2) continue;
+    const long wgs = (units + n - 1) / n, t = ((wgs + cus - 1) / cus) * cost[n - 2];
+    if (n == 8 || t < least) {
+      least = t;
+      per_wg = n;
+    }
+  }
+  return per_wg;
+}
+
 }  // namespace spd

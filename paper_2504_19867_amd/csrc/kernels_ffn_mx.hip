@@ -6,6 +6,7 @@
 // scale byte of its 32 entries.  Weights are the A operand, so that a lane has consecutive outputs of one token.  Where the E2M1 lane of row r
 // and quarter c of a step of 128 entries holds the entries 32 c .. 32 c + 31, the E4M3 lane holds 16 c .. 16 c + 15 and 64 + 16 c ..
 // 64 + 16 c + 15: that is the order in which the instruction multiplies; the scales go by quarters in both.
+#include "ffn_stream.h"
 #include "ffn_tiles.h"
 #include "mx.h"
 
@@ -21,6 +22,8 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x2_any __attribute__((ext_vector_type(2), aligned(2)));   // `out` is only promised to be aligned to its entries
 
 __device__ inline uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
@@ -125,31 +128,143 @@ __global__ __launch_bounds__(256) void ffn_unpack_mx_kernel(const char* __restri
   }
 }
 
-// grid (inter / 16 * token blocks of 16), block 64: a wave computes 16 outputs of 16 tokens, operands straight from memory.
-__global__ __launch_bounds__(64) void ffn_gate_up_mx_kernel(const char* __restrict__ x, const uint32_t* __restrict__ xs, const char* __restrict__ w,
-                                                            bf16_t* __restrict__ out, int T, int K, int I, StepMark mark) {
+// Up to 128 tokens: bound by reading the weights once.  They go straight from memory into operand registers (a load is 1 KiB of consecutive
+// bytes, 16 rows x 128 entries, and 128 bytes of scales), every wave streaming the gate and up rows of 16 outputs, or a part of their entries,
+// through a ring of RING slices of 128 entries that no barrier touches.  All 16 NB tokens' rows, which the waves share, go through LDS, XS slices
+// at a time in two stages, loaded a stage ahead: a barrier per XS slices.  A workgroup has UNITS x SPLIT waves: UNITS of 16 outputs, the entries of
+// each in SPLIT parts, whose sums meet in LDS at the end (ffn_mx_stream_units says which).
+// 1 token of hidden 4096, inter 14336 takes 12.4 us on 128 CUs and 9.8 on 256 (5.0 and 6.4 TB/s, weights from HBM), 64 tokens 16 and 14, 128 tokens
+// 27 and 19: from there on operand reads from LDS and the matrix instructions take as long as the weights.  Weights through a ring in LDS,
+// filled by loads that go straight there: 12.4, at 64 tokens 19 us on 128 CUs.  Rings of eight slices, or x pieces in smaller stages: slower.
+template <int NB, int UNITS, int SPLIT, int RING, int XS>
+__global__ __launch_bounds__(64 * UNITS * SPLIT, 1) void ffn_gate_up_mx_stream_kernel(const char* __restrict__ x, const uint32_t* __restrict__ xs,
+                                                                                    const char* __restrict__ w, bf16_t* __restrict__ out, int T, int K,
+                                                                                    int I, StepMark mark) {
   if (blockIdx.x == 0 && threadIdx.x == 0) store_mark(mark);
-  const int lane = threadIdx.x, n16 = lane & 15, c4 = lane >> 4, n_kt = K / 128;
-  const int unit = blockIdx.x % (I / 16), t = blockIdx.x / (I / 16) * 16 + n16, tc = min(t, T - 1);
-  const char* wt = w + (size_t)(unit >> 3) * n_kt * FFN_MX_TILE_BYTES;
-  const char* codes = wt + (unit & 7) * 2048 + lane * 16;
-  const char* scales = wt + SCALES_AT + (unit & 7) * 128 + n16 * 8;
-  const char* xr = x + (size_t)tc * K + 16 * c4;
-  f32x4 g = {0.f, 0.f, 0.f, 0.f}, u = g;
-  for (int kt = 0; kt < n_kt; ++kt) {
-    const size_t at = (size_t)kt * FFN_MX_TILE_BYTES;
-    const u32x4 wg = *(const u32x4*)(codes + at), wu = *(const u32x4*)(codes + at + 1024);
-    const uint2 s = *(const uint2*)(scales + at);
-    const uint32_t sx = xs[(size_t)kt * T + tc] >> (8 * c4);
-    const i32x8 xv = e4m3_operand(*(const u32x4*)(xr + kt * 128), *(const u32x4*)(xr + kt * 128 + 64));
-    g = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(e2m1_operand(wg), xv, g, E2M1, E4M3, 0, (int)(s.x >> (8 * c4)), 0, (int)sx);
-    u = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(e2m1_operand(wu), xv, u, E2M1, E4M3, 0, (int)(s.y >> (8 * c4)), 0, (int)sx);
+  constexpr int WAVES = UNITS * SPLIT, THREADS = 64 * WAVES, ROWS = 16 * NB;
+  constexpr int PIECES = SPLIT * XS * ROWS * 8, XL = (PIECES + THREADS - 1) / THREADS;   // 16-byte pieces of a stage, per thread
+  constexpr int WORDS = SPLIT * XS * ROWS, SL = (WORDS + THREADS - 1) / THREADS;         // scale words of a stage
+  constexpr int SLICE = ROWS * 128, X_STAGE = SPLIT * XS * SLICE, STAGE = X_STAGE + WORDS * 4;
+  static_assert(RING % XS == 0, "whole stages per ring");
+  static_assert((SPLIT - 1) * UNITS * 2 * NB * 1024 <= 2 * STAGE, "room for the parts' sums");
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n16 = lane & 15, c4 = lane >> 4;
+  const int n_slices = K / 128, per_part = (n_slices + SPLIT - 1) / SPLIT;
+  const int part = wave / UNITS, first = part * per_part, mine = min(per_part, n_slices - first);
+  // (waves of the last workgroup without outputs of their own repeat the last ones and store nothing)
+  const int n_units = I / 16, unit = (int)blockIdx.x * UNITS + wave % UNITS, u = min(unit, n_units - 1);
+  const char* wt = w + (size_t)(u >> 3) * n_slices * FFN_MX_TILE_BYTES;
+  const uint32_t code_off = (uint32_t)((u & 7) * 2048 + lane * 16), scale_off = (uint32_t)(SCALES_AT + (u & 7) * 128 + n16 * 8);
+  struct Slice { u32x4 g, u; u32x2 s; };
+  auto load_w = [&](int s) __attribute__((always_inline)) -> Slice {
+    const char* t = wt + (size_t)min(first + s, n_slices - 1) * FFN_MX_TILE_BYTES;
+    return Slice{__builtin_nontemporal_load((const u32x4*)(t + code_off)), __builtin_nontemporal_load((const u32x4*)(t + code_off + 1024)),
+                 __builtin_nontemporal_load((const u32x2*)(t + scale_off))};
+  };
+  // piece i of a stage: chunk i % 8 of row i / 8 % ROWS of slice i / (8 ROWS) % XS of part i / (8 ROWS XS); rows past T re-read row T - 1, slices
+  // past the last one that one.  Slot s of a row of 128 bytes holds the row's chunk s ^ ((row >> 1) & 7): 16 rows then lie in all banks.
+  u32x4 xr[XL];
+  uint32_t sr[SL];
+  auto slice_of = [&](int st, int q) __attribute__((always_inline)) -> int { return min(q / XS * per_part + st * XS + q % XS, n_slices - 1); };
+  auto load_x = [&](int st) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < XL; ++j) {
+      const int i = min(tid + THREADS * j, PIECES - 1), row = i / 8 % ROWS;
+      xr[j] = *(const u32x4*)(x + (uint32_t)(min(row, T - 1) * K + slice_of(st, i / (8 * ROWS)) * 128 + i % 8 * 16));
+    }
+#pragma unroll
+    for (int j = 0; j < SL; ++j) {
+      const int i = min(tid + THREADS * j, WORDS - 1);
+      sr[j] = xs[(uint32_t)(slice_of(st, i / ROWS) * T + min(i % ROWS, T - 1))];
+    }
+  };
+  auto store_x = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < XL; ++j) {
+      const int i = tid + THREADS * j, row = i / 8 % ROWS;
+      if (PIECES % THREADS == 0 || i < PIECES) *(u32x4*)(smem + buf * STAGE + i / 8 * 128 + ((i % 8) ^ ((row >> 1) & 7)) * 16) = xr[j];
+    }
+#pragma unroll
+    for (int j = 0; j < SL; ++j) {
+      const int i = tid + THREADS * j;
+      if (WORDS % THREADS == 0 || i < WORDS) *(uint32_t*)(smem + buf * STAGE + X_STAGE + i * 4) = sr[j];
+    }
+  };
+  f32x4 acc[2][NB];
+#pragma unroll
+  for (int a = 0; a < 2; ++a)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  Slice wr[RING];
+  load_x(0);
+  store_x(0);
+  // the next x pieces before the weights, as inside the loop: the compiler then waits for them with the weights still on their way
+  load_x(1);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int s = 0; s < RING; ++s) wr[s] = load_w(s);
+  int buf = 0;
+  const int sw = (n16 >> 1) & 7, x0 = part * XS * SLICE + n16 * 128 + (c4 ^ sw) * 16, x1 = part * XS * SLICE + n16 * 128 + ((4 + c4) ^ sw) * 16;
+  const int s_at = X_STAGE + part * XS * ROWS * 4 + n16 * 4 + c4;
+  const int n_stages = (per_part + XS - 1) / XS;
+  // RING slices from s0 on, with the loads of the next RING; `tail`: of both, those that there are
+  auto round = [&](int s0, auto tail) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < RING; ++r) {
+      if (r % XS == 0) {
+        // everyone's pieces of this stage are there, and everyone is done with the one before, which the next pieces replace
+        __syncthreads();
+        store_x(buf ^ 1);
+        __builtin_amdgcn_sched_barrier(0);
+        if (!tail || (s0 + r) / XS + 2 < n_stages) load_x((s0 + r) / XS + 2);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      const char* st = smem + buf * STAGE;
+      if (!tail || s0 + r < mine) {
+        const int sg = (int)(wr[r].s.x >> (8 * c4)), su = (int)(wr[r].s.y >> (8 * c4));
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const i32x8 xv = e4m3_operand(*(const u32x4*)(st + x0 + r % XS * SLICE + b * 2048), *(const u32x4*)(st + x1 + r % XS * SLICE + b * 2048));
+          const int sx = *(const uint8_t*)(st + s_at + r % XS * ROWS * 4 + b * 64);
+          acc[0][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(e2m1_operand(wr[r].g), xv, acc[0][b], E2M1, E4M3, 0, sg, 0, sx);
+          acc[1][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(e2m1_operand(wr[r].u), xv, acc[1][b], E2M1, E4M3, 0, su, 0, sx);
+          if (b == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (!tail || s0 + r + RING < mine) wr[r] = load_w(s0 + r + RING);
+      __builtin_amdgcn_sched_barrier(0);
+      if (r % XS == XS - 1) buf ^= 1;
+    }
+  };
+  int s0 = 0;
+  const int whole = n_slices - (SPLIT - 1) * per_part;            // slices that every part has: fewer than some
+  for (; s0 + 2 * RING <= whole; s0 += RING) round(s0, std::false_type{});
+  for (; s0 < per_part; s0 += RING) round(s0, std::true_type{});
+  if constexpr (SPLIT > 1) {                      // the parts' sums, through LDS, to the first, which adds them up in order
+    __syncthreads();
+    f32x4* const sums = (f32x4*)smem + lane;
+    if (part > 0) {
+#pragma unroll
+      for (int i = 0; i < 2 * NB; ++i) sums[(((part - 1) * UNITS + wave % UNITS) * 2 * NB + i) * 64] = acc[i / NB][i % NB];
+    }
+    __syncthreads();
+    if (part > 0) return;
+#pragma unroll
+    for (int p = 0; p < SPLIT - 1; ++p)
+#pragma unroll
+      for (int i = 0; i < 2 * NB; ++i) acc[i / NB][i % NB] += sums[((p * UNITS + wave) * 2 * NB + i) * 64];
   }
-  // element i of lane (n16, c4) is output 4 c4 + i of token n16
-  if (t >= T) return;
-  const uint32_t y0 = pack_bf16(silu(g[0]) * u[0], silu(g[1]) * u[1]), y1 = pack_bf16(silu(g[2]) * u[2], silu(g[3]) * u[3]);
-  bf16_t* o = out + (size_t)t * I + unit * 16 + 4 * c4;
-  o[0] = (bf16_t)y0; o[1] = (bf16_t)(y0 >> 16); o[2] = (bf16_t)y1; o[3] = (bf16_t)(y1 >> 16);
+  // element i of lane (n16, c4) is output 4 c4 + i of token n16 of its block
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int t = 16 * b + n16;
+    const uint32_t y0 = pack_bf16(silu(acc[0][b][0]) * acc[1][b][0], silu(acc[0][b][1]) * acc[1][b][1]);
+    const uint32_t y1 = pack_bf16(silu(acc[0][b][2]) * acc[1][b][2], silu(acc[0][b][3]) * acc[1][b][3]);
+    if (t < T && unit < n_units) *(u32x2_any*)(out + (size_t)t * I + unit * 16 + 4 * c4) = u32x2_any{y0, y1};
+  }
 }
 
 // 256 tokens x 128 outputs (256 rows of weights).  As ffn_gate_up_large_kernel: eight waves in two groups that run half a step apart, one group's
@@ -368,6 +483,29 @@ __global__ __launch_bounds__(512, 2) void ffn_gate_up_mx_large_kernel(const char
   if (!wm) barrier();                             // as many as the second group
 }
 
+template <int NB>
+static hipError_t launch_mx_stream(const void* x, const void* x_scales, const void* w_mx, void* out, int T, int K, int I, int cus, const StepMark& mark,
+                                   hipStream_t stream) {
+  auto launch = [&](auto kernel, int units, int split) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((I / 16 + units - 1) / units)), dim3((unsigned)(64 * units * split)), 0, stream, (const char*)x,
+                       (const uint32_t*)x_scales, (const char*)w_mx, (bf16_t*)out, T, K, I, mark);
+  };
+  const int units = ffn_mx_stream_units(NB, I / 16, cus);
+  if constexpr (NB <= 4) {
+    if (units == 7) launch(ffn_gate_up_mx_stream_kernel<NB, 7, 1, 4, 4>, 7, 1);
+    if (units == 6) launch(ffn_gate_up_mx_stream_kernel<NB, 6, 1, 4, 4>, 6, 1);
+    if (units == 5) launch(ffn_gate_up_mx_stream_kernel<NB, 5, 1, 4, 4>, 5, 1);
+    if (units == 4) launch(ffn_gate_up_mx_stream_kernel<NB, 4, 1, 4, 4>, 4, 1);
+    if (units == 3) launch(ffn_gate_up_mx_stream_kernel<NB, 3, 2, 4, 4>, 3, 2);
+    if (units == 2) launch(ffn_gate_up_mx_stream_kernel<NB, 2, 2, 4, 4>, 2, 2);
+  } else {
+    if (units == 4) launch(ffn_gate_up_mx_stream_kernel<NB, 4, 2, 4, 2>, 4, 2);
+    if (units == 2) launch(ffn_gate_up_mx_stream_kernel<NB, 2, 2, 4, 2>, 2, 2);
+  }
+  if (units == 8) launch(ffn_gate_up_mx_stream_kernel<NB, 8, 1, 4, 4>, 8, 1);
+  return hipGetLastError();
+}
+
 hipError_t launch_ffn_gate_up_mx(const void* x, const void* x_scales, const void* w_mx, void* out, int T, int K, int I, int xcds, int cus, bool exclusive,
                                  const StepMark& mark, hipStream_t stream) {
   if (T > 128) {
@@ -381,11 +519,10 @@ hipError_t launch_ffn_gate_up_mx(const void* x, const void* x_scales, const void
                        (bf16_t*)out, T, K, I, tiles_m, tiles_n, xcds, mark);
     return hipGetLastError();
   }
-  const int64_t wgs = (int64_t)(I / 16) * ((T + (int64_t)15) / 16);
-  if (wgs > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(ffn_gate_up_mx_kernel, dim3((unsigned)wgs), dim3(64), 0, stream, (const char*)x, (const uint32_t*)x_scales, (const char*)w_mx,
-                     (bf16_t*)out, T, K, I, mark);
-  return hipGetLastError();
+  if (T <= 16) return launch_mx_stream<1>(x, x_scales, w_mx, out, T, K, I, cus, mark, stream);
+  if (T <= 32) return launch_mx_stream<2>(x, x_scales, w_mx, out, T, K, I, cus, mark, stream);
+  if (T <= 64) return launch_mx_stream<4>(x, x_scales, w_mx, out, T, K, I, cus, mark, stream);
+  return launch_mx_stream<8>(x, x_scales, w_mx, out, T, K, I, cus, mark, stream);
 }
 
 static unsigned pack_grid(long n_pieces) { return (unsigned)std::min<long>((n_pieces + 255) / 256, 8192); }

@@ -131,6 +131,23 @@ def test_shares_of_the_chip(ctx, cus, T, I, K):
     c.close()
 
 
+@pytest.mark.parametrize("T", [3, 20, 50, 100])
+@pytest.mark.parametrize("I", [128, 1408, 2048, 2560, 2816, 3584, 4096, 4224])
+def test_units_per_workgroup(T, I):
+    """On 32 compute units: workgroups of two to eight units of 16 outputs, whole and not; slices that divide evenly over waves and rings and not."""
+    c = S.Context(0)
+    c.set_partition(c.device_info()[0] - 32, 32)
+    rng = np.random.default_rng(I + T)
+    for K in (128, 896, 1152):
+        wg, wu = _weights(rng, I, K)
+        w = _pack(c, DEC, wg, wu)
+        x, b = _rows(rng, T, K)
+        got = _run(c, DEC, *mx_tensors(x, b), w, T, K, I)
+        pick = sorted({0, T // 2, T - 1})
+        _check(got[pick], x[pick], *(mx.quantise(v, mx.E2M1)[0] for v in (wg, wu)))
+    c.close()
+
+
 @pytest.mark.parametrize("T", [1, 48, 300])
 def test_model_shape(ctx, T):
     """hidden 4096, inter 14336: sampled outputs of all tokens"""
