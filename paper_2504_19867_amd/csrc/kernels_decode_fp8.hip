@@ -5,8 +5,11 @@
 // exact in bf16, so that the products are those of the values that codes and scales stand for, and the queries keep their bf16.
 //   S^T[key, query] = K_tile[16 x d] . Q^T[d x 16]       v_mfma_f32_16x16x32_bf16, d/32 steps for each of two tiles
 //   O^T[dim, query] += V^T[16 x 32] . P^T[32 x 16]       v_mfma_f32_16x16x32_bf16, d/16 blocks for both tiles together
-// Bound by memory: 2 d + 1/4 bytes per token and KV head.  A wave streams its tiles through a ring of registers, the scales of its next 64
-// tiles come by one load (one tile per lane) and from there by lane reads.
+// Bound by memory: 2 d + 1/4 bytes per token and KV head.  A wave streams its tiles through two steps' registers, the scales of its next 64
+// tiles come by one load (one tile per lane) and from there by lane reads.  What is in registers bounds the workgroups of a compute unit, and
+// three with two steps hide one another's starts and ends better than two with four (64 requests of 512 .. 4096 tokens, 8 KV heads of 128 dims, on
+// 128 CUs 75.8 / 83.1 us, 128 lognormal ones of 64 query heads 139 / 147, six workgroups per compute unit dealt).  With two dealt (split_gqa) 69.4
+// and 137: 4.8 TB/s inside the attention launch, where a plain read through registers has 5.5; over bf16 pages 122 and 234.
 #include "decode_gqa.h"
 #include "gqa_fp8_tile.h"
 #include "internal.h"
@@ -121,7 +124,7 @@ __device__ inline void compute_step8(const Step8<D>& f, const uint32_t (&sc)[2],
 // grid (n_items * n_kv_heads), block 256, as decode_gqa_kernel.  WHOLE: the launch rotates and appends too (the wave whose step holds the new
 // token's block changes it in registers, on its way into the matrix cores, and puts it back); otherwise decode_prepare_fp8_kernel has.
 template <int D, bool WHOLE>
-__global__ __launch_bounds__(256, 2) void decode_gqa_fp8_kernel(GqaArgs a) {
+__global__ __launch_bounds__(256, 3) void decode_gqa_fp8_kernel(GqaArgs a) {
   if constexpr (!WHOLE) {
     a.rot = 0;
     a.k_new = nullptr;
@@ -198,14 +201,20 @@ __global__ __launch_bounds__(256, 2) void decode_gqa_fp8_kernel(GqaArgs a) {
     if (a.rot && lane < PCS) kv_oth = *(const uint4*)(src + rope_partner(e0, a.off, a.rot, interleaved));
   }
 
-  constexpr int RING = 4;                          // steps in registers
+  constexpr int RING = 2;                          // steps in registers
   Step8<D> f[RING];
   TileWindow win = TileWindow{0, 0};
+  // Where the steady state is reached its first loads are unconditional: the compiler then knows how many are on their way behind a
+  // step's, and waits for that step's alone.
+  constexpr int STEADY = 2 * RING - 1;
+  const bool many_steps = my_steps >= STEADY;
   if (my_steps > 0) {
     win = fill_window(0);
+    if (!many_steps) {
 #pragma unroll
-    for (int i = 0; i < RING - 1; ++i)
-      if (i < my_steps) load_step8<D>(f[i], pool_g, win, i, lane);
+      for (int i = 0; i < RING - 1; ++i)
+        if (i < my_steps) load_step8<D>(f[i], pool_g, win, i, lane);
+    }
   }
   if (a.rot) {
     if (lane < (a.rot >> 1)) {
@@ -256,28 +265,35 @@ __global__ __launch_bounds__(256, 2) void decode_gqa_fp8_kernel(GqaArgs a) {
     }
     compute_step8<D>(s, sc, qf, O, m, l, tile, n, a.c, c4);
   };
-  for (int s0 = 0; s0 < my_steps; s0 += 32) {      // 32 steps (of 128 tokens over the four waves) per window
-    const int s1 = min(my_steps, s0 + 32);
-    if (s0) {
-      win = fill_window(s0);
+  // steps i .. s1 - 1, fewer than 2 RING, their first RING - 1 on their way
+  auto rest = [&](int i, int s0, int s1) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < RING - 1; ++i)
-        if (s0 + i < s1) load_step8<D>(f[i], pool_g, win, i, lane);
-    }
-    int i = s0;
-    while (i + 2 * RING - 2 < s1) {                // (all loads of the round are there, and its steps are not the last)
-#pragma unroll
-      for (int r = 0; r < RING; ++r) {
-        load_step8<D>(f[(r + RING - 1) % RING], pool_g, win, i + r + RING - 1 - s0, lane);
-        compute(f[r], i + r, s0, false);
-      }
-      i += RING;
-    }
-#pragma unroll
-    for (int r = 0; r < 2 * RING; ++r) {
+    for (int r = 0; r < 2 * RING - 1; ++r) {
       if (i + r >= s1) break;
       if (i + r + RING - 1 < s1) load_step8<D>(f[(r + RING - 1) % RING], pool_g, win, i + r + RING - 1 - s0, lane);
       compute(f[r % RING], i + r, s0, i + r == my_steps - 1);
+    }
+  };
+  if (!many_steps) {
+    rest(0, 0, my_steps);
+  } else {
+    for (int s0 = 0; s0 < my_steps; s0 += 32) {    // 32 steps (of 128 tokens over the four waves) per window
+      const int s1 = min(my_steps, s0 + 32);
+      if (s0) win = fill_window(s0);
+      // (steps past the request's end are its last tile again)
+#pragma unroll
+      for (int i = 0; i < RING - 1; ++i) load_step8<D>(f[i], pool_g, win, i, lane);
+      int i = s0;
+      while (i + STEADY <= s1) {
+#pragma unroll
+        for (int r = 0; r < RING; ++r) {
+          load_step8<D>(f[(r + RING - 1) % RING], pool_g, win, i + r + RING - 1 - s0, lane);
+          __builtin_amdgcn_sched_barrier(0);
+          compute(f[r], i + r, s0, false);
+        }
+        i += RING;
+      }
+      rest(i, s0, s1);
     }
   }
   l += __shfl_xor(l, 16);
@@ -319,7 +335,9 @@ __global__ __launch_bounds__(256, 2) void decode_gqa_fp8_kernel(GqaArgs a) {
 }
 
 // Rotation of the queries into q_rot and the append of the new tokens, ahead of an attention launch of many workgroups (as
-// decode_prepare_kernel).  grid (n_items), block 256: the workgroup of a request's last chunk does the request, a wave per KV head in turn.
+// decode_prepare_kernel).  grid (n_items, 1 + n_kv_heads / 4), block 256: the workgroups of a request's last chunk do the request, the first the
+// queries, each of the others four KV heads, a wave each.  Bound by latency (record, then rows and block): all a wave's loads go out together, and
+// the angles are formed meanwhile.  200 requests, 32 query and 8 KV heads on 128 CUs: 7.0 us, with all of a request in one workgroup 10.3.
 template <int D>
 __global__ __launch_bounds__(256) void decode_prepare_fp8_kernel(GqaArgs a, bf16_t* __restrict__ q_rot) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -331,48 +349,66 @@ __global__ __launch_bounds__(256) void decode_prepare_fp8_kernel(GqaArgs a, bf16
   const int b = head[0], n = head[3], n_tiles = (n + TILE_T - 1) / TILE_T;
   if (head[4] + head[5] != n_tiles) return;        // not the request's last chunk
   const bool interleaved = a.interleaved != 0;
-  constexpr int PCS = D / 8;
-  if (a.rot) {
+  constexpr int PCS = D / 8, BATCH = 4;            // 16-byte pieces of a head; loads on their way per thread
+  auto angles = [&]() __attribute__((always_inline)) {
     if (tid < (a.rot >> 1)) {
       const double turns = (double)(n - 1) * w * 0.15915494309189535;
       const float ang = (float)((turns - __builtin_rint(turns)) * 6.283185307179586);
       sincosf(ang, &sn[tid], &cs[tid]);
     }
     __syncthreads();
+  };
+  if (blockIdx.y == 0) {
+    if (!a.rot) return;
     const bf16_t* q = a.q + (size_t)b * a.H * D;
     bf16_t* to = q_rot + (size_t)b * a.H * D;
-    for (int i = tid; i < a.H * PCS; i += 256) {
-      const int e0 = 8 * (i % PCS);
-      const uint4 own = *(const uint4*)(q + 8 * i), oth = *(const uint4*)(q + i / PCS * D + rope_partner(e0, a.off, a.rot, interleaved));
-      *(uint4*)(to + 8 * i) = rope_rotate(own, oth, e0, a.off, a.rot, interleaved, cs, sn);
+    const int n_q = a.H * PCS;
+    uint4 own[BATCH], oth[BATCH];
+    auto load = [&](int i0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) {
+        const int i = min(i0 + 256 * j, n_q - 1);
+        own[j] = *(const uint4*)(q + 8 * i);
+        oth[j] = *(const uint4*)(q + i / PCS * D + rope_partner(8 * (i % PCS), a.off, a.rot, interleaved));
+      }
+    };
+    load(tid);
+    angles();
+    for (int i0 = tid; i0 < n_q; i0 += 256 * BATCH) {
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) {
+        const int i = i0 + 256 * j;
+        if (i < n_q) *(uint4*)(to + 8 * i) = rope_rotate(own[j], oth[j], 8 * (i % PCS), a.off, a.rot, interleaved, cs, sn);
+      }
+      load(i0 + 256 * BATCH);
     }
+    return;
   }
   if (!a.k_new) return;
-  const int sub = (n_tiles - 1) % a.tiles_per_page;
+  const int g = 4 * ((int)blockIdx.y - 1) + wave, gc = min(g, a.Hkv - 1), sub = (n_tiles - 1) % a.tiles_per_page;   // (a wave without a head stores nothing)
   char* page = a.pool + (uint64_t)(uint32_t)last_page * a.page_bytes;
+  char* tile = page + (uint64_t)gc * a.head_bytes + (uint64_t)sub * a.tile_bytes;
+  char* scale_at = page + a.scale_off + 2 * ((uint64_t)gc * a.tiles_per_page + sub);
   bf16_t *krow = rows[wave][0], *vrow = rows[wave][1];
-  for (int g = wave; g < a.Hkv; g += 4) {
-    char* tile = page + (uint64_t)g * a.head_bytes + (uint64_t)sub * a.tile_bytes;
-    char* scale_at = page + a.scale_off + 2 * ((uint64_t)g * a.tiles_per_page + sub);
-    uint4 k[D / 64], v[D / 64];
+  const int pc = lane % PCS, e0 = 8 * pc;
+  const bf16_t* src = (lane / PCS & 1 ? a.v_new : a.k_new) + ((size_t)b * a.Hkv + gc) * D;   // lanes 0 .. PCS - 1: pieces of the key, the next PCS: of the value
+  uint4 piece = *(const uint4*)(src + e0), oth = uint4{0, 0, 0, 0};
+  if (a.rot) oth = *(const uint4*)(src + rope_partner(e0, a.off, a.rot, interleaved));
+  uint4 k[D / 64], v[D / 64];
 #pragma unroll
-    for (int p = 0; p < D / 64; ++p) {
-      k[p] = *((const uint4*)tile + p * 64 + lane);
-      v[p] = *((const uint4*)(tile + TILE_T * D) + p * 64 + lane);
-    }
-    const uint32_t sc = *(const unsigned short*)scale_at;
-    if (lane < 2 * PCS) {
-      const int pc = lane % PCS, e0 = 8 * pc;
-      const bf16_t* src = (lane < PCS ? a.k_new : a.v_new) + ((size_t)b * a.Hkv + g) * D;
-      uint4 piece = *(const uint4*)(src + e0);
-      if (a.rot && lane < PCS) piece = rope_rotate(piece, *(const uint4*)(src + rope_partner(e0, a.off, a.rot, interleaved)), e0, a.off, a.rot, interleaved, cs, sn);
-      *(uint4*)((lane < PCS ? krow : vrow) + e0) = piece;
-    }
-    lds_visible_in_wave();
-    const uint32_t now = append_token<D>(k, v, sc, (n - 1) % TILE_T, krow, vrow, lane);
-    store_block<D>(tile, scale_at, k, v, now, lane);
-    lds_visible_in_wave();                         // the rows have been read: the next head's may replace them
+  for (int p = 0; p < D / 64; ++p) {
+    k[p] = *((const uint4*)tile + p * 64 + lane);
+    v[p] = *((const uint4*)(tile + TILE_T * D) + p * 64 + lane);
   }
+  const uint32_t sc = *(const unsigned short*)scale_at;
+  if (a.rot) {
+    angles();
+    if (lane < PCS) piece = rope_rotate(piece, oth, e0, a.off, a.rot, interleaved, cs, sn);
+  }
+  if (lane < 2 * PCS) *(uint4*)((lane < PCS ? krow : vrow) + e0) = piece;
+  lds_visible_in_wave();
+  const uint32_t now = append_token<D>(k, v, sc, (n - 1) % TILE_T, krow, vrow, lane);
+  if (g < a.Hkv) store_block<D>(tile, scale_at, k, v, now, lane);
 }
 
 template <int D>
@@ -393,8 +429,9 @@ hipError_t launch_decode_gqa_fp8(const PoolGeom& g, char* pool_base, const Decod
 
 hipError_t launch_decode_prepare_fp8(const PoolGeom& g, char* pool_base, const DecodeLaunch& d, int n_items, void* q_rot, hipStream_t stream) {
   const GqaArgs a = gqa_args(g, pool_base, d);
-  if (g.dk == 128) hipLaunchKernelGGL(decode_prepare_fp8_kernel<128>, dim3((unsigned)n_items), dim3(256), 0, stream, a, (bf16_t*)q_rot);
-  else if (g.dk == 64) hipLaunchKernelGGL(decode_prepare_fp8_kernel<64>, dim3((unsigned)n_items), dim3(256), 0, stream, a, (bf16_t*)q_rot);
+  const dim3 grid((unsigned)n_items, (unsigned)(1 + (d.k_new ? (g.Hkv + 3) / 4 : 0)));
+  if (g.dk == 128) hipLaunchKernelGGL(decode_prepare_fp8_kernel<128>, grid, dim3(256), 0, stream, a, (bf16_t*)q_rot);
+  else if (g.dk == 64) hipLaunchKernelGGL(decode_prepare_fp8_kernel<64>, grid, dim3(256), 0, stream, a, (bf16_t*)q_rot);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
