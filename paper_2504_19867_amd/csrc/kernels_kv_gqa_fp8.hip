@@ -6,10 +6,9 @@
 // A step whose attention reads dense rows wants a block's earlier rows as they were before the new ones came: the wave that writes the
 // block hands them out too, since nobody else may read it meanwhile.
 //
-// One launch does what a call or a step does to rows: the page write of the new ones (with the rotation of the keys, and the rows as they are for
-// a step whose attention reads dense rows), cached rows to dense ones, and the copy of the step's metadata.  A wave takes a block: its lane (t, c)
-// has the token t and of every 32 entries of the head the eight from 8 c on, which for keys is the page's order.  Values lie in the page with four
-// tokens of an entry together: the four lanes of a quad turn 4 x 4 bytes round among themselves, and the words cross LDS.
+// A wave takes a block (of a few KV heads of a tile in turn).  Rows are moved in row order, 16 bytes per lane of whole rows; codes change between
+// row order and page order in LDS, as rows of codes.  Values lie in the page with four tokens of an entry together: there the four lanes of
+// a quad turn 4 x 4 bytes round among themselves.
 // Bound by memory (4 d + 2 d bytes per token and head either way).
 #include "gqa_fp8_tile.h"
 #include "rope_device.h"
@@ -43,218 +42,221 @@ struct Rows8Args {
   uint32_t head_bytes, tile_bytes;
   int tiles_per_page, Hkv;
   const TileDesc* descs;
-  int n_tiles, HG, groups;       // HG: KV heads per workgroup
+  int HG, groups;                // KV heads per workgroup, workgroups per tile
   const bf16_t *k, *v;
-  bf16_t* k_rw;                  // k again, where the keys are rotated
   int n_copy;
   uint4* copy_dst;
   const uint4* copy_src;
   uint64_t copy_n16;
-  const TileDesc* cached;
-  int n_cached;
   bf16_t *k_all, *v_all;
-  const double* w;
-  int rot, off, interleaved;
   StepMark mark;
 };
 }  // namespace
 
-template <int D, bool ROPE>
-__global__ __launch_bounds__(256) void kv_rows_gqa_fp8_kernel(Rows8Args a) {
-  int blk = blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if (blk == 0 && tid == 0) store_mark(a.mark);
-  if (blk < a.n_copy) {
-    for (uint64_t j = (uint64_t)blk * 256 + tid; j < a.copy_n16; j += (uint64_t)a.n_copy * 256) a.copy_dst[j] = a.copy_src[j];
-    return;
+// What a wave knows of its tile (one descriptor per workgroup) and of its place in it.
+template <int D>
+struct Place {
+  static constexpr int NP = D / 64, PCS = D / 8, STEP = 64 / PCS, NR = 16 / STEP;   // pieces of a row; rows of one load instruction, instructions of a block
+  static constexpr int PITCH = D + 8;              // bytes of a row of codes in LDS
+  const Rows8Args& a;
+  TileDesc d;
+  int lane, col, c4;                               // page order: token (keys) or entry (values), quarter or token quad
+  int piece, row0;                                 // row order: the lane's entries are 8 piece .. + 7 of the rows row0 + STEP r
+  int g_begin, g_end;
+  char *lds, *page;
+  // Rows of [rows][Hkv][D] tensors: a wave-uniform address of the head's row `row` (of token slot 0, which may lie ahead of the tensor where
+  // that slot is not touched) and of every STEP rows from there, and the lane's bytes behind it.
+  uint32_t row_off;
+  int64_t row_step;
+  __device__ Place(const Rows8Args& args, int blk, char* codes_lds) : a(args), d(args.descs[blk / args.groups]) {
+    d.src_row = __builtin_amdgcn_readfirstlane(d.src_row); d.page = __builtin_amdgcn_readfirstlane(d.page); d.sub = __builtin_amdgcn_readfirstlane(d.sub);
+    d.t_begin = __builtin_amdgcn_readfirstlane(d.t_begin); d.t_end = __builtin_amdgcn_readfirstlane(d.t_end);
+    d.pad[0] = __builtin_amdgcn_readfirstlane(d.pad[0]); d.pad[1] = __builtin_amdgcn_readfirstlane(d.pad[1]);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    lane = threadIdx.x & 63; col = lane & 15; c4 = lane >> 4; piece = lane % PCS; row0 = lane / PCS;
+    g_begin = blk % a.groups * a.HG + wave; g_end = min(blk % a.groups * a.HG + a.HG, a.Hkv);   // (every fourth head: a wave's)
+    lds = codes_lds + wave * (16 * PITCH);
+    page = a.base + (uint64_t)d.page * a.page_bytes;
+    row_off = (uint32_t)(row0 * a.Hkv * D + 8 * piece) * 2;
+    row_step = (int64_t)STEP * a.Hkv * D * 2;
   }
-  blk -= a.n_copy;
-  constexpr int NP = D / 64, QUAD = 80;            // a token quad's 16 pieces of 16 bytes in LDS, in words, with room between
-  __shared__ __attribute__((aligned(16))) uint32_t turn[4][NP * 4 * QUAD];
-  __shared__ float cs[ROPE ? 16 * (D / 2 + 1) : 1], sn[ROPE ? 16 * (D / 2 + 1) : 1];
-  const int col = lane & 15, c4 = lane >> 4;
-  uint32_t* lds = turn[wave];
-  // where in LDS this lane's words belong: after the turn, entry 64 p + 32 h + 8 c4 + 4 e + (col & 3) of the tokens 4 (col / 4) .. + 3
-  auto word_at = [&](int p, int h, int e) -> int {
-    const int d = 32 * h + 8 * c4 + 4 * e + (col & 3);
-    return (p * 4 + (col >> 2)) * QUAD + (d & 15) * 4 + (d >> 4);
-  };
-  const bool write = blk < a.n_tiles * a.groups;
-  if (!write) blk -= a.n_tiles * a.groups;
-  const TileDesc d = (write ? a.descs : a.cached)[blk / a.groups];
-  const int g_begin = blk % a.groups * a.HG, g_end = min(g_begin + a.HG, a.Hkv);
-  const bool mine = col >= d.t_begin && col < d.t_end;
-  char* page = a.base + (uint64_t)d.page * a.page_bytes;
-
-  // the block k, v, as it lies in its page, to dense rows: token t to row row0 + t, where `wanted`
-  auto hand_out = [&](const uint4 (&k)[NP], const uint4 (&v)[NP], uint32_t scales, int row0, int g, bool wanted) __attribute__((always_inline)) {
-    const float ks = scale_of(scales & 255), vs = scale_of(scales >> 8);
-#pragma unroll
-    for (int p = 0; p < NP; ++p) *(uint4*)(lds + (p * 4 + c4) * QUAD + col * 4) = v[p];
-    lds_visible_in_wave();
-    const size_t row = ((size_t)(row0 + col) * a.Hkv + g) * D;
+  __device__ char* tile(int g) const { return page + (uint64_t)g * a.head_bytes + (uint64_t)d.sub * a.tile_bytes; }
+  __device__ char* scales(int g) const { return page + a.scale_off + 2 * ((uint64_t)g * a.tiles_per_page + d.sub); }
+  __device__ char* rows(const void* p, int row, int g) const { return (char*)p + ((int64_t)row * a.Hkv + g) * (D * 2); }
+  __device__ int token(int r) const { return row0 + STEP * r; }
+  __device__ bool touched(int r) const { return token(r) >= d.t_begin && token(r) < d.t_end; }
+  // the block of head g as bf16 to dense rows: token t to row dense0 + t, for first <= t < last
+  __device__ __attribute__((always_inline)) void hand_out(int dense0, int g, int first, int last) const {
+    uint4 b[2][NP];
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      const uint32_t kw[4] = {k[p].x, k[p].y, k[p].z, k[p].w};
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t x = turn_quad(lds[word_at(p, h, 0)], col & 3), y = turn_quad(lds[word_at(p, h, 1)], col & 3);
-        if (wanted) {
-          *(uint4*)(a.k_all + row + 64 * p + 32 * h + 8 * c4) = widen_row(kw[2 * h], kw[2 * h + 1], ks);
-          *(uint4*)(a.v_all + row + 64 * p + 32 * h + 8 * c4) = widen_row(x, y, vs);
-        }
-      }
+      b[0][p] = load_once((const uint4*)tile(g) + p * 64 + lane);
+      b[1][p] = load_once((const uint4*)(tile(g) + TILE_T * D) + p * 64 + lane);
     }
-    lds_visible_in_wave();
-  };
-
-  if (write) {
-    if constexpr (ROPE) {
-      const int half = a.rot >> 1;
-      for (int i = tid; i < 16 * half; i += 256) {
-        const int t = i / half, pair = i % half;
-        const double turns = (double)(d.pad[0] + t) * a.w[pair] * 0.15915494309189535;   // angle / 2 pi
-        const float r = (float)((turns - __builtin_rint(turns)) * 6.283185307179586);
-        sincosf(r, &sn[t * (D / 2 + 1) + pair], &cs[t * (D / 2 + 1) + pair]);
-      }
-      __syncthreads();
-    }
-    for (int g = g_begin + wave; g < g_end; g += 4) {
-      const size_t row = ((size_t)(d.src_row + col - d.t_begin) * a.Hkv + g) * D;
-      char* tile = page + (uint64_t)g * a.head_bytes + (uint64_t)d.sub * a.tile_bytes;
-      char* scale_at = page + a.scale_off + 2 * ((uint64_t)g * a.tiles_per_page + d.sub);
-      uint4 k[2 * NP], v[2 * NP], oth[2 * NP], k_old[NP], v_old[NP];
-      uint32_t scales = 0;
+    const uint32_t sc = *(const unsigned short*)scales(g);
 #pragma unroll
-      for (int s = 0; s < 2 * NP; ++s) {
-        k[s] = v[s] = oth[s] = uint4{0, 0, 0, 0};
-        if (mine) {
-          const int e0 = 32 * s + 8 * c4;
-          k[s] = *(const uint4*)(a.k + row + e0);
-          v[s] = *(const uint4*)(a.v + row + e0);
-          if constexpr (ROPE) oth[s] = *(const uint4*)(a.k + row + rope_partner(e0, a.off, a.rot, a.interleaved != 0));
+    for (int side = 0; side < 2; ++side) {
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {               // rows of codes in LDS
+        const uint32_t w[4] = {b[side][p].x, b[side][p].y, b[side][p].z, b[side][p].w};
+        if (side == 0) {
+          *(uint2*)(lds + col * PITCH + 64 * p + 8 * c4) = uint2{w[0], w[1]};
+          *(uint2*)(lds + col * PITCH + 64 * p + 32 + 8 * c4) = uint2{w[2], w[3]};
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) *(uint32_t*)(lds + (4 * c4 + (col & 3)) * PITCH + 64 * p + 16 * i + (col & ~3)) = turn_quad(w[i], col & 3);
         }
       }
-      if (d.t_begin > 0) {
-        scales = *(const unsigned short*)scale_at;
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          k_old[p] = *((const uint4*)tile + p * 64 + lane);
-          v_old[p] = *((const uint4*)(tile + TILE_T * D) + p * 64 + lane);
-        }
-      }
-      if constexpr (ROPE) {
-        const float *c = cs + col * (D / 2 + 1), *si = sn + col * (D / 2 + 1);
-#pragma unroll
-        for (int s = 0; s < 2 * NP; ++s) k[s] = rope_rotate(k[s], oth[s], 32 * s + 8 * c4, a.off, a.rot, a.interleaved != 0, c, si);
-      }
-      uint32_t mk = 0, mv = 0;
-#pragma unroll
-      for (int s = 0; s < 2 * NP; ++s) {
-        mk = max(max(mk, max(finite_magnitude_bf16x2(k[s].x), finite_magnitude_bf16x2(k[s].y))), max(finite_magnitude_bf16x2(k[s].z), finite_magnitude_bf16x2(k[s].w)));
-        mv = max(max(mv, max(finite_magnitude_bf16x2(v[s].x), finite_magnitude_bf16x2(v[s].y))), max(finite_magnitude_bf16x2(v[s].z), finite_magnitude_bf16x2(v[s].w)));
-      }
-      uint32_t bk = scale_byte_e4m3(wave_max(mk)), bv = scale_byte_e4m3(wave_max(mv));
-      const uint32_t ok = scales & 255, ov = scales >> 8;
-      if (d.t_begin > 0) {
-        bk = max(bk, ok);
-        bv = max(bv, ov);
-      }
-      const float ik = inverse_scale_of(bk), iv = inverse_scale_of(bv);
-      auto codes = [](uint32_t x, uint32_t y, float f) -> uint32_t {
-        return e4m3_codes(rope_bf_lo(x) * f, rope_bf_hi(x) * f, rope_bf_lo(y) * f, rope_bf_hi(y) * f);
-      };
-      // rows as they are (rotated keys), where somebody wants them
-      if (mine) {
-        const size_t dense = ((size_t)(d.pad[1] + col - d.t_begin) * a.Hkv + g) * D;
-#pragma unroll
-        for (int s = 0; s < 2 * NP; ++s) {
-          if constexpr (ROPE) *(uint4*)(a.k_rw + row + 32 * s + 8 * c4) = k[s];
-          if (a.k_all) {
-            *(uint4*)(a.k_all + dense + 32 * s + 8 * c4) = k[s];
-            *(uint4*)(a.v_all + dense + 32 * s + 8 * c4) = v[s];
-          }
-        }
-      }
-      if (a.k_all && d.t_begin > 0) hand_out(k_old, v_old, scales, d.pad[1] - d.t_begin, g, col < d.t_begin);
-#pragma unroll
-      for (int p = 0; p < NP; ++p)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint4 x = v[2 * p + h];
-          lds[word_at(p, h, 0)] = turn_quad(codes(x.x, x.y, iv), col & 3);
-          lds[word_at(p, h, 1)] = turn_quad(codes(x.z, x.w, iv), col & 3);
-        }
       lds_visible_in_wave();
+      const float f = scale_of(side == 0 ? sc & 255 : sc >> 8);
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        const int t = token(r);
+        const uint2 c = *(const uint2*)(lds + t * PITCH + 8 * piece);
+        if (t >= first && t < last) *(uint4*)(rows(side == 0 ? a.k_all : a.v_all, dense0, g) + r * row_step + row_off) = widen_row(c.x, c.y, f);
+      }
+      lds_visible_in_wave();
+    }
+  }
+};
+
+// grid (n_tiles * groups), block 256: cached rows to dense ones, the values that codes and scales stand for, exact in bf16.  A kernel of its own: it
+// needs a quarter of the registers of the page write, and what its workgroups wait for (descriptor, then block) is hidden by their number: 16001
+// rows of 8 heads of 128 dims 28 us on 128 CUs (3.5 TB/s), in one kernel with the page write 40.
+template <int D>
+__global__ __launch_bounds__(256, 8) void kv_read_gqa_fp8_kernel(Rows8Args a) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) store_mark(a.mark);
+  __shared__ __attribute__((aligned(16))) char codes_lds[4 * 16 * Place<D>::PITCH];
+  const Place<D> at(a, blockIdx.x, codes_lds);
+  for (int g = at.g_begin; g < at.g_end; g += 4) at.hand_out(at.d.src_row - at.d.t_begin, g, at.d.t_begin, at.d.t_end);
+}
+
+// grid (n_copy + n_tiles * groups), block 256: the page write, the rows as they are to dense ones, and the copy of the step's metadata.  9000 rows of 8
+// heads of 128 dims 19 us on 128 CUs (2.9 TB/s).  Rotating the keys on the way as the bf16 page write does was slower than the rotation's own launch
+// (2500 rows: 26 us instead of 9, which that launch, busy with the queries anyway, takes 3 us longer): the angles' code holds the registers.
+template <int D>
+__global__ __launch_bounds__(256, 4) void kv_write_gqa_fp8_kernel(Rows8Args a) {
+  const int tid = threadIdx.x;
+  if (blockIdx.x == 0 && tid == 0) store_mark(a.mark);
+  if ((int)blockIdx.x < a.n_copy) {
+    for (uint64_t j = (uint64_t)blockIdx.x * 256 + tid; j < a.copy_n16; j += (uint64_t)a.n_copy * 256) a.copy_dst[j] = a.copy_src[j];
+    return;
+  }
+  using P = Place<D>;
+  constexpr int NP = P::NP, NR = P::NR, PITCH = P::PITCH;
+  __shared__ __attribute__((aligned(16))) char codes_lds[4 * 16 * PITCH];
+  const P at(a, (int)blockIdx.x - a.n_copy, codes_lds);
+  const TileDesc& d = at.d;
+  const int e0 = 8 * at.piece, col = at.col, c4 = at.c4;
+  char* const lds = at.lds;
+  for (int g = at.g_begin; g < at.g_end; g += 4) {
+    uint4 k[NR], v[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      k[r] = v[r] = uint4{0, 0, 0, 0};
+      if (at.touched(r)) {
+        k[r] = load_once((const uint4*)(at.rows(a.k, d.src_row - d.t_begin, g) + r * at.row_step + at.row_off));
+        v[r] = load_once((const uint4*)(at.rows(a.v, d.src_row - d.t_begin, g) + r * at.row_step + at.row_off));
+      }
+    }
+    uint32_t mk = 0, mv = 0, before = 0;
+    if (d.t_begin > 0) before = *(const unsigned short*)at.scales(g);
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      mk = max(max(mk, max(finite_magnitude_bf16x2(k[r].x), finite_magnitude_bf16x2(k[r].y))), max(finite_magnitude_bf16x2(k[r].z), finite_magnitude_bf16x2(k[r].w)));
+      mv = max(max(mv, max(finite_magnitude_bf16x2(v[r].x), finite_magnitude_bf16x2(v[r].y))), max(finite_magnitude_bf16x2(v[r].z), finite_magnitude_bf16x2(v[r].w)));
+    }
+    uint32_t bk = scale_byte_e4m3(wave_max(mk)), bv = scale_byte_e4m3(wave_max(mv));
+    const uint32_t ok = before & 255, ov = before >> 8;
+    if (d.t_begin > 0) {
+      bk = max(bk, ok);
+      bv = max(bv, ov);
+    }
+    if (a.k_all) {                                 // rows as they are, where somebody wants them
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        if (at.touched(r)) {
+          *(uint4*)(at.rows(a.k_all, d.pad[1] - d.t_begin, g) + r * at.row_step + at.row_off) = k[r];
+          *(uint4*)(at.rows(a.v_all, d.pad[1] - d.t_begin, g) + r * at.row_step + at.row_off) = v[r];
+        }
+      }
+    }
+    if (a.k_all && d.t_begin > 0) at.hand_out(d.pad[1] - d.t_begin, g, 0, d.t_begin);
+    char* tile = at.tile(g);
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+      __builtin_amdgcn_sched_barrier(0);
+      const float f = inverse_scale_of(side == 0 ? bk : bv);
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {               // rows of codes in LDS
+        const uint4 y = side == 0 ? k[r] : v[r];
+        *(uint2*)(lds + at.token(r) * PITCH + e0) =
+            uint2{e4m3_codes(rope_bf_lo(y.x) * f, rope_bf_hi(y.x) * f, rope_bf_lo(y.y) * f, rope_bf_hi(y.y) * f),
+                  e4m3_codes(rope_bf_lo(y.z) * f, rope_bf_hi(y.z) * f, rope_bf_lo(y.w) * f, rope_bf_hi(y.w) * f)};
+      }
+      lds_visible_in_wave();
+      const uint32_t was = side == 0 ? ok : ov, now = side == 0 ? bk : bv;
+      const float grown = __builtin_bit_cast(float, (uint32_t)max(127 + (int)was - (int)now, 0) << 23);
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
-        uint32_t kw[4] = {codes(k[2 * p].x, k[2 * p].y, ik), codes(k[2 * p].z, k[2 * p].w, ik), codes(k[2 * p + 1].x, k[2 * p + 1].y, ik),
-                          codes(k[2 * p + 1].z, k[2 * p + 1].w, ik)};
-        const uint4 x = *(const uint4*)(lds + (p * 4 + c4) * QUAD + col * 4);
-        uint32_t vw[4] = {x.x, x.y, x.z, x.w};
-        if (d.t_begin > 0) {                       // the rows ahead stay, under the block's scale as it is now
-          const uint32_t ko[4] = {k_old[p].x, k_old[p].y, k_old[p].z, k_old[p].w}, vo[4] = {v_old[p].x, v_old[p].y, v_old[p].z, v_old[p].w};
-          const float fk = __builtin_bit_cast(float, (uint32_t)max(127 + (int)ok - (int)bk, 0) << 23);
-          const float fv = __builtin_bit_cast(float, (uint32_t)max(127 + (int)ov - (int)bv, 0) << 23);
-          const int in = d.t_begin - 4 * c4;       // bytes of a word of values that stay
-          const uint32_t keep = in <= 0 ? 0 : in >= 4 ? ~0u : (1u << (8 * in)) - 1;
+        uint32_t w[4];
+        if (side == 0) {
+          const uint2 lo = *(const uint2*)(lds + col * PITCH + 64 * p + 8 * c4), hi = *(const uint2*)(lds + col * PITCH + 64 * p + 32 + 8 * c4);
+          w[0] = lo.x; w[1] = lo.y; w[2] = hi.x; w[3] = hi.y;
+        } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (col < d.t_begin) kw[i] = bk != ok ? recode(ko[i], fk) : ko[i];
-            vw[i] = (vw[i] & ~keep) | ((bv != ov ? recode(vo[i], fv) : vo[i]) & keep);
-          }
+          for (int i = 0; i < 4; ++i) w[i] = turn_quad(*(const uint32_t*)(lds + (4 * c4 + (col & 3)) * PITCH + 64 * p + 16 * i + (col & ~3)), col & 3);
         }
-        store_once((uint4*)tile + p * 64 + lane, uint4{kw[0], kw[1], kw[2], kw[3]});
-        store_once((uint4*)(tile + TILE_T * D) + p * 64 + lane, uint4{vw[0], vw[1], vw[2], vw[3]});
-      }
-      if (lane == 0) *(unsigned short*)scale_at = (unsigned short)(bk | bv << 8);
-      lds_visible_in_wave();                       // (the next head's words replace this one's)
-    }
-    return;
-  }
-
-  // cached rows: the values that codes and scales stand for, exact in bf16
-  for (int g = g_begin + wave; g < g_end; g += 4) {
-    const char* tile = page + (uint64_t)g * a.head_bytes + (uint64_t)d.sub * a.tile_bytes;
-    const uint32_t scales = *(const unsigned short*)(page + a.scale_off + 2 * ((uint64_t)g * a.tiles_per_page + d.sub));
-    uint4 k[NP], v[NP];
+        if (d.t_begin > 0) {                       // the rows ahead stay, under the block's scale as it is now
+          const uint4 o = *((const uint4*)(tile + side * TILE_T * D) + p * 64 + at.lane);
+          const uint32_t ow[4] = {o.x, o.y, o.z, o.w};
+          const int in = d.t_begin - 4 * c4;       // bytes of a word of values that stay
+          const uint32_t keep = side == 0 ? (col < d.t_begin ? ~0u : 0) : in <= 0 ? 0 : in >= 4 ? ~0u : (1u << (8 * in)) - 1;
 #pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      k[p] = load_once((const uint4*)tile + p * 64 + lane);
-      v[p] = load_once((const uint4*)(tile + TILE_T * D) + p * 64 + lane);
+          for (int i = 0; i < 4; ++i) w[i] = (w[i] & ~keep) | ((now != was ? recode(ow[i], grown) : ow[i]) & keep);
+        }
+        store_once((uint4*)(tile + side * TILE_T * D) + p * 64 + at.lane, uint4{w[0], w[1], w[2], w[3]});
+      }
+      lds_visible_in_wave();
     }
-    hand_out(k, v, scales, d.src_row - d.t_begin, g, mine);
+    if (at.lane == 0) *(unsigned short*)at.scales(g) = (unsigned short)(bk | bv << 8);
   }
 }
 
+// KV heads per workgroup: one per wave, unless there are so many tiles that workgroups queue for compute units; then the reads of the descriptors, which
+// may lie in pinned host memory, are worth halving.
+static int heads_per_workgroup(int n_tiles, int Hkv, int cus) { return (int64_t)n_tiles * ((Hkv + 3) / 4) <= 4 * (int64_t)cus ? 4 : 8; }
+
 hipError_t launch_kv_rows_gqa_fp8(const PoolGeom& g, char* pool_base, const TileDesc* d_tiles, int n_tiles, const void* k, const void* v,
                                   const KvRows& x, const StepMark& mark, hipStream_t stream) {
-  if (x.q) return hipErrorInvalidValue;            // (the queries' rotation is a launch of its own)
+  if (x.rope_w) return hipErrorInvalidValue;       // (the rotation is a launch of its own)
   Rows8Args a{};
   a.base = pool_base;
   a.page_bytes = g.page_bytes; a.scale_off = g.scale_off; a.head_bytes = g.head_bytes; a.tile_bytes = g.tile_bytes;
   a.tiles_per_page = g.tiles_per_page; a.Hkv = g.Hkv;
-  a.descs = d_tiles; a.n_tiles = n_tiles;
-  a.HG = 4; a.groups = (g.Hkv + a.HG - 1) / a.HG;
-  a.k = (const bf16_t*)k; a.v = (const bf16_t*)v; a.k_rw = (bf16_t*)const_cast<void*>(k);
+  a.k = (const bf16_t*)k; a.v = (const bf16_t*)v;
   a.copy_dst = (uint4*)x.copy_dst; a.copy_src = (const uint4*)x.copy_src;
   a.copy_n16 = x.copy_dst ? (x.copy_bytes + 15) / 16 : 0;
   a.n_copy = (int)std::min<uint64_t>(128, (a.copy_n16 + 255) / 256);
-  a.cached = x.d_cached; a.n_cached = x.n_cached; a.k_all = (bf16_t*)x.k_all; a.v_all = (bf16_t*)x.v_all;
-  a.w = x.rope_w; a.rot = x.rot; a.off = x.off; a.interleaved = x.interleaved ? 1 : 0;
+  a.k_all = (bf16_t*)x.k_all; a.v_all = (bf16_t*)x.v_all;
   a.mark = mark;
-  const int64_t blocks = a.n_copy + ((int64_t)n_tiles + a.n_cached) * a.groups;
-  if (blocks <= 0) return hipSuccess;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a); };
-  if (g.dk == 128) {
-    if (x.rope_w) launch(kv_rows_gqa_fp8_kernel<128, true>);
-    else launch(kv_rows_gqa_fp8_kernel<128, false>);
-  } else {
-    if (x.rope_w) launch(kv_rows_gqa_fp8_kernel<64, true>);
-    else launch(kv_rows_gqa_fp8_kernel<64, false>);
-  }
-  return hipGetLastError();
+  // what is done to `tiles` tiles, `copying` workgroups ahead of them
+  auto launch = [&](auto kernel, int tiles, int copying) -> hipError_t {
+    a.HG = heads_per_workgroup(tiles, g.Hkv, x.cus); a.groups = (g.Hkv + a.HG - 1) / a.HG;
+    const int64_t blocks = copying + (int64_t)tiles * a.groups;
+    if (blocks <= 0) return hipSuccess;
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a);
+    a.mark.flag = nullptr;
+    return hipGetLastError();
+  };
+  a.descs = d_tiles;
+  hipError_t e;
+  if (g.dk == 128) e = launch(kv_write_gqa_fp8_kernel<128>, n_tiles, a.n_copy);
+  else e = launch(kv_write_gqa_fp8_kernel<64>, n_tiles, a.n_copy);
+  if (e != hipSuccess) return e;
+  a.descs = x.d_cached;
+  return g.dk == 128 ? launch(kv_read_gqa_fp8_kernel<128>, x.n_cached, 0) : launch(kv_read_gqa_fp8_kernel<64>, x.n_cached, 0);
 }
 
 }  // namespace spd

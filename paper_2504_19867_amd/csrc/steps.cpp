@@ -323,7 +323,11 @@ extern "C" int spd_prefill_step(spd_ctx* ctx, spd_pool* pool, const spd_prefill_
     KvRows x;
     x.cus = share;
     x.copy_dst = ws; x.copy_src = st->dev; x.copy_bytes = bytes;
-    if (rc_) {
+    if (rc_ && eight) {                             // (queries and keys by a launch of their own)
+      SPD_HIP(launch_rope((void*)b->q, b->n_q_heads, (void*)b->k, b->n_kv_heads, b->dim_qk, rc_->rotary_dim, rc_->rotary_offset,
+                          rc_->interleaved != 0, n_rows, (const int32_t*)(st->dev + off_pos), rope_w, mark, stream));
+      mark.flag = nullptr;
+    } else if (rc_) {
       x.rope_w = rope_w; x.rot = rc_->rotary_dim; x.off = rc_->rotary_offset; x.interleaved = rc_->interleaved != 0;
       if (!own_rope) { x.q = (void*)b->q; x.n_q_heads = b->n_q_heads; }
     }
@@ -332,7 +336,7 @@ extern "C" int spd_prefill_step(spd_ctx* ctx, spd_pool* pool, const spd_prefill_
       x.k_all = rows_k; x.v_all = rows_v;
     }
     SPD_HIP(launch_kv_rows(g, pool->base, d_desc, (int)n_descs, page_src_k, page_src_v, x, mark, stream));
-    if (own_rope)
+    if (own_rope && !eight)
       SPD_HIP(launch_rope((void*)b->q, b->n_q_heads, nullptr, 0, b->dim_qk, rc_->rotary_dim, rc_->rotary_offset,
                           rc_->interleaved != 0, n_rows, (const int32_t*)(ws + off_pos), rope_w, StepMark{}, stream));
   } else {
