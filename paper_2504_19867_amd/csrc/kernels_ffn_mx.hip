@@ -250,16 +250,20 @@ __global__ __launch_bounds__(64 * UNITS * SPLIT, 1) void ffn_gate_up_mx_stream_k
   }
 }
 
-// 256 tokens x 128 outputs (256 rows of weights).  As ffn_gate_up_large_kernel: eight waves in two groups that run half a step apart, one group's
+// 64 MB tokens x 128 outputs (256 rows of weights).  As ffn_gate_up_large_kernel: eight waves in two groups that run half a step apart, one group's
 // matrix instructions beside the other group's loads and operand reads, an s_barrier at every change; a workgroup walks the tiles slot, slot +
-// gridDim / xcds, .. with its loads running ahead across tiles.  A step is 64 hidden entries, 8 v_mfma_scale_f32_32x32x64 per wave, 512 cycles at the
+// gridDim / xcds, .. with its loads running ahead across tiles.  A step is 64 hidden entries, 2 MB v_mfma_scale_f32_32x32x64 per wave, 128 MB cycles at the
 // rate of the 8-bit operand; both operands' bytes come in pairs of steps (128 entries: whole cache lines of x, a tile of the packed weights), three
-// pairs in LDS: 3 x (32 KiB x, 16 KiB codes of weights, 1 KiB of scales of either).
+// pairs in LDS: 3 x (8 MB KiB x, 16 KiB codes of weights, 1 KiB of scales of either).
+// MB is 4, or 2 where half as many tokens per tile fill the share better (low_tiles_pay).
+// Bound by the matrix instructions: 8192 tokens of hidden 4096, inter 14336 on 128 compute units 892 us, 2.16 PFLOP/s, 86% of what 64 cycles per
+// instruction allow at 2.4 GHz; 4096 tokens 475 us, on 256 compute units 312 (3.1 PFLOP/s).
+template <int MB>
 __global__ __launch_bounds__(512, 2) void ffn_gate_up_mx_large_kernel(const char* __restrict__ x, const uint32_t* __restrict__ xs, const char* __restrict__ w,
                                                                       bf16_t* __restrict__ out, int T, int K, int I, int tiles_m, int tiles_n, int xcds,
                                                                       StepMark mark) {
   if (blockIdx.x == 0 && threadIdx.x == 0) store_mark(mark);
-  constexpr int BM = 256, X_PAIR = BM * 128, W_PAIR = SCALES_AT, S_PAIR = 2048, NP = 3;   // bytes of a pair, pairs in LDS
+  constexpr int BM = 64 * MB, JX = MB / 2, X_PAIR = BM * 128, W_PAIR = SCALES_AT, S_PAIR = 2048, NP = 3;   // bytes of a pair, pairs in LDS
   constexpr int W_LDS = NP * X_PAIR, S_LDS = W_LDS + NP * W_PAIR;
   __shared__ __attribute__((aligned(1024))) char smem[S_LDS + NP * S_PAIR];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -274,11 +278,11 @@ __global__ __launch_bounds__(512, 2) void ffn_gate_up_mx_large_kernel(const char
   const int n_pairs = K / 128, n_steps = 2 * n_pairs;
   int left = ((n_slots - 1 - slot) / slot_step + 1) * n_steps;   // steps of all tiles of this workgroup from the current one on
 
-  // ---- loads, in two halves of a pair: 128 rows of x (two instructions per wave; slot s of a row of 128 bytes holds the row's chunk
-  // s ^ ((row >> 1) & 7)) and four units of the weights (one); with the first half the scales (one: waves 0 .. 3 the tokens', 4 .. 7 the weights').
-  // Token rows past T re-read row T - 1.
+  // ---- loads, in two halves of a pair: half the rows of x (JX instructions per wave; slot s of a row of 128 bytes holds the row's chunk
+  // s ^ ((row >> 1) & 7)) and four units of the weights (one); with the first half the scales (one: waves 0 .. 3 the tokens', of 128 tokens twice,
+  // 4 .. 7 the weights').  Token rows past T re-read row T - 1.
   const int x_chunk = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7);
-  uint32_t x_voff[2][2], s_voff;                  // [half][j]
+  uint32_t x_voff[2][JX], s_voff;                  // [half][j]
   const uint32_t w_voff = (uint32_t)lane * 16;
   const char *x_ptr, *w_ptr, *s_ptr;              // the next pair's
   size_t s_step;                                  // of s_ptr, from pair to pair
@@ -289,14 +293,14 @@ __global__ __launch_bounds__(512, 2) void ffn_gate_up_mx_large_kernel(const char
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        x_voff[hf][j] = (uint32_t)min(128 * hf + 8 * (wave + 8 * j) + (lane >> 3), T - 1 - tm * BM) * (uint32_t)K + (uint32_t)x_chunk * 16;
+      for (int j = 0; j < JX; ++j)
+        x_voff[hf][j] = (uint32_t)min(BM / 2 * hf + 8 * (wave + 8 * j) + (lane >> 3), T - 1 - tm * BM) * (uint32_t)K + (uint32_t)x_chunk * 16;
     x_ptr = x + (size_t)(tm * BM) * K;
     w_ptr = w + (size_t)tn * n_pairs * FFN_MX_TILE_BYTES + wave * 1024;
     if (wave < 4) {
       s_ptr = (const char*)(xs + tm * BM);
       s_step = (size_t)T * 4;
-      s_voff = (uint32_t)min(64 * wave + lane, T - 1 - tm * BM) * 4;
+      s_voff = (uint32_t)min(64 * (wave % MB) + lane, T - 1 - tm * BM) * 4;
     } else {
       s_ptr = w + (size_t)tn * n_pairs * FFN_MX_TILE_BYTES + SCALES_AT;
       s_step = FFN_MX_TILE_BYTES;
@@ -307,10 +311,10 @@ __global__ __launch_bounds__(512, 2) void ffn_gate_up_mx_large_kernel(const char
   auto load = [&](int stage, int hf) __attribute__((always_inline)) {
     const uint32_t lds = smem_base + stage * X_PAIR + hf * (X_PAIR / 2) + wave * 1024;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) dma16s(x_ptr, x_voff[hf][j], lds + j * 8192);
+    for (int j = 0; j < JX; ++j) dma16s(x_ptr, x_voff[hf][j], lds + j * 8192);
     dma16s(w_ptr + hf * 8192, w_voff, smem_base + W_LDS + stage * W_PAIR + hf * 8192 + wave * 1024);
     if (hf == 0) {
-      dma4s(s_ptr, s_voff, smem_base + S_LDS + stage * S_PAIR + wave * 256);
+      dma4s(s_ptr, s_voff, smem_base + S_LDS + stage * S_PAIR + (wave < 4 ? wave % MB : wave) * 256);
     } else {
       x_ptr += 128;
       w_ptr += FFN_MX_TILE_BYTES;
@@ -331,20 +335,20 @@ __global__ __launch_bounds__(512, 2) void ffn_gate_up_mx_large_kernel(const char
   for (int j = 0; j < 2; ++j)
 #pragma unroll
     for (int sl = 0; sl < 2; ++sl) {
-      x_off[0][sl][j] = (wm * 128 + n32) * 128 + ((4 * sl + 2 * j + hh) ^ ((n32 >> 1) & 7)) * 16;
+      x_off[0][sl][j] = (wm * (BM / 2) + n32) * 128 + ((4 * sl + 2 * j + hh) ^ ((n32 >> 1) & 7)) * 16;
       x_off[1][sl][j] = x_off[0][sl][j] + 2 * X_PAIR;
       asm volatile("" : "+v"(x_off[1][sl][j]));   // a value of its own, not "x_off + constant" to be recomputed
     }
   const int unit = 2 * wn + (n32 >> 4), row = n32 & 15;
-  int w_off = W_LDS + unit * 2048 + hh * 256 + row * 16, ws_off = S_LDS + 1024 + unit * 128 + row * 8, xs_off = S_LDS + (wm * 128 + n32) * 4;
+  int w_off = W_LDS + unit * 2048 + hh * 256 + row * 16, ws_off = S_LDS + 1024 + unit * 128 + row * 8, xs_off = S_LDS + (wm * (BM / 2) + n32) * 4;
   asm volatile("" : "+v"(w_off), "+v"(ws_off), "+v"(xs_off));
-  u32x4 ox[4][2], ow[2];
-  uint32_t sx[4], sw[2];                          // scale bytes: of the pair's first step in byte 0, of its second in byte 2
+  u32x4 ox[MB][2], ow[2];
+  uint32_t sx[MB], sw[2];                         // scale bytes: of the pair's first step in byte 0, of its second in byte 2
   // acc[mb][0] = gate, acc[mb][1] = up: element i of lane (n32, hh) is output 8 (i / 4) + 4 hh + i % 4 of token 32 mb + n32
-  f32x16 acc[4][2];
+  f32x16 acc[MB][2];
   auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int mb = 0; mb < 4; ++mb)
+    for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
       for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
@@ -363,7 +367,7 @@ __global__ __launch_bounds__(512, 2) void ffn_gate_up_mx_large_kernel(const char
   if (left > 2) {
     load(1, 0);
     load(1, 1);
-    SPD_WAIT_VMCNT(7);
+    SPD_WAIT_VMCNT(2 * JX + 3);
   } else {
     SPD_WAIT_VMCNT(0);
   }
@@ -383,37 +387,37 @@ __global__ __launch_bounds__(512, 2) void ffn_gate_up_mx_large_kernel(const char
       const uint2 two = *(const uint2*)(smem + ws_off + P * S_PAIR);
       sw[0] = two.x; sw[1] = two.y;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sx[r] = *(const uint32_t*)(smem + xs_off + P * S_PAIR + r * 128);
+      for (int r = 0; r < MB; ++r) sx[r] = *(const uint32_t*)(smem + xs_off + P * S_PAIR + r * 128);
     }
 #pragma unroll
     for (int r = 0; r < 2; ++r) ow[r] = *(const u32x4*)(smem + w_off + P * W_PAIR + SL * 512 + r * 1024);
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < MB; ++r)
 #pragma unroll
       for (int j = 0; j < 2; ++j) ox[r][j] = *(const u32x4*)(smem + x_off[P == 2][SL][j] + (P == 1 ? X_PAIR : 0) + r * (32 * 128));
     __builtin_amdgcn_sched_barrier(0);
     if (ready > 0) --ready;
-    else if (left >= 5) SPD_WAIT_VMCNT(7);        // this step's loads and those of the one before: three and four
-    else if (left == 4) SPD_WAIT_VMCNT(3);
+    else if (left >= 5) SPD_WAIT_VMCNT(2 * JX + 3);   // this step's loads and those of the one before
+    else if (left == 4) SPD_WAIT_VMCNT(JX + 1);
     else SPD_WAIT_VMCNT(0);
     __builtin_amdgcn_s_waitcnt(0xc07f);           // lgkmcnt(0)
     if constexpr (SL == 0) {
 #pragma unroll
       for (int r = 0; r < 2; ++r) sw[r] >>= 8 * hh;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sx[r] >>= 8 * hh;
+      for (int r = 0; r < MB; ++r) sx[r] >>= 8 * hh;
     }
     barrier();
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int mb = 0; mb < 4; ++mb)
+    for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
       for (int nb = 0; nb < 2; ++nb)
         acc[mb][nb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(e2m1_operand(ow[nb]), e4m3_operand(ox[mb][0], ox[mb][1]), acc[mb][nb], E2M1, E4M3,
                                                                       2 * SL, (int)sw[nb], 2 * SL, (int)sx[mb]);
     // (the products belong here: without side effects of their own they would be moved past the barriers to where their sums are used)
 #pragma unroll
-    for (int mb = 0; mb < 4; ++mb) asm volatile("" : "+v"(acc[mb][0]), "+v"(acc[mb][1]));
+    for (int mb = 0; mb < MB; ++mb) asm volatile("" : "+v"(acc[mb][0]), "+v"(acc[mb][1]));
     __builtin_amdgcn_s_setprio(0);
     barrier();
     --left;
@@ -426,13 +430,13 @@ __global__ __launch_bounds__(512, 2) void ffn_gate_up_mx_large_kernel(const char
     int tm, tn;
     order.tile(slot, tm, tn);
 #pragma unroll
-    for (int mb = 0; mb < 4; ++mb) {
+    for (int mb = 0; mb < MB; ++mb) {
       uint32_t y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         y[i] = pack_bf16(silu(acc[mb][0][2 * i]) * acc[mb][1][2 * i], silu(acc[mb][0][2 * i + 1]) * acc[mb][1][2 * i + 1]);
       if (mb == 0) SPD_WAIT_VMCNT(0);
-      const int t = tm * BM + wm * 128 + mb * 32 + n32;
+      const int t = tm * BM + wm * (BM / 2) + mb * 32 + n32;
       bf16_t* o = out + (size_t)t * I + tn * 128 + wn * 32 + 8 * hh;
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
@@ -489,19 +493,34 @@ static hipError_t launch_mx_stream(const void* x, const void* x_scales, const vo
   return hipGetLastError();
 }
 
+template <int MB>
+static hipError_t launch_mx_tiles(const void* x, const void* x_scales, const void* w_mx, void* out, int T, int K, int I, int xcds, int cus, bool exclusive,
+                                  const StepMark& mark, hipStream_t stream) {
+  const int tiles_m = (int)(((int64_t)T + 64 * MB - 1) / (64 * MB)), tiles_n = I / 128;
+  const int persistent = exclusive ? cus : 0;      // workgroups, one per compute unit of a share that has them to itself; 0: one per tile
+  if (tiles_n < xcds || persistent % xcds) xcds = 1;
+  int64_t n = xcds > 1 ? (int64_t)((tiles_n + xcds - 1) / xcds) * tiles_m * xcds : (int64_t)tiles_m * tiles_n;
+  if (n > INT32_MAX) return hipErrorInvalidValue;
+  if (persistent) n = std::min<int64_t>(n, persistent);
+  hipLaunchKernelGGL(ffn_gate_up_mx_large_kernel<MB>, dim3((unsigned)n), dim3(512), 0, stream, (const char*)x, (const uint32_t*)x_scales, (const char*)w_mx,
+                     (bf16_t*)out, T, K, I, tiles_m, tiles_n, xcds, mark);
+  return hipGetLastError();
+}
+
+// Whether tiles of 128 tokens are to be taken instead of 256.  One round of them, a tile per compute unit, takes 0.70 .. 0.75 of the time of one of the larger
+// ones, which are fed from LDS once for twice the products, and every further round 0.65; three rounds for two are a tie.  256 / 128 tokens
+// per tile: hidden 4096, inter 14336 on 256 CUs, 256 tokens (1 round either) 43.3 / 32.4 us, 512 (1, 2) 47.2 / 59.2, 700 (2, 3) 82.9 / 80.5, 8192 on 128 CUs (28, 56)
+// 892 / 1200; 300 on 96 CUs (3, 4) 105 / 94; hidden 4096, inter 3584 on 128 CUs, 512 (1, 1) 38.3 / 28.4.
+static bool low_tiles_pay(int T, int I, int cus) {
+  const int64_t columns = I / 128, high = (((int64_t)T + 255) / 256 * columns + cus - 1) / cus, low = (((int64_t)T + 127) / 128 * columns + cus - 1) / cus;
+  return 2 * low < 3 * high;
+}
+
 hipError_t launch_ffn_gate_up_mx(const void* x, const void* x_scales, const void* w_mx, void* out, int T, int K, int I, int xcds, int cus, bool exclusive,
                                  const StepMark& mark, hipStream_t stream) {
-  if (T > 128) {
-    const int tiles_m = (int)(((int64_t)T + 255) / 256), tiles_n = I / 128;
-    const int persistent = exclusive ? cus : 0;    // workgroups, one per compute unit of a share that has them to itself; 0: one per tile
-    if (tiles_n < xcds || persistent % xcds) xcds = 1;
-    int64_t n = xcds > 1 ? (int64_t)((tiles_n + xcds - 1) / xcds) * tiles_m * xcds : (int64_t)tiles_m * tiles_n;
-    if (n > INT32_MAX) return hipErrorInvalidValue;
-    if (persistent) n = std::min<int64_t>(n, persistent);
-    hipLaunchKernelGGL(ffn_gate_up_mx_large_kernel, dim3((unsigned)n), dim3(512), 0, stream, (const char*)x, (const uint32_t*)x_scales, (const char*)w_mx,
-                       (bf16_t*)out, T, K, I, tiles_m, tiles_n, xcds, mark);
-    return hipGetLastError();
-  }
+  if (T > 128)
+    return low_tiles_pay(T, I, cus) ? launch_mx_tiles<2>(x, x_scales, w_mx, out, T, K, I, xcds, cus, exclusive, mark, stream)
+                                    : launch_mx_tiles<4>(x, x_scales, w_mx, out, T, K, I, xcds, cus, exclusive, mark, stream);
   if (T <= 16) return launch_mx_stream<1>(x, x_scales, w_mx, out, T, K, I, cus, mark, stream);
   if (T <= 32) return launch_mx_stream<2>(x, x_scales, w_mx, out, T, K, I, cus, mark, stream);
   if (T <= 64) return launch_mx_stream<4>(x, x_scales, w_mx, out, T, K, I, cus, mark, stream);

@@ -131,6 +131,22 @@ def test_shares_of_the_chip(ctx, cus, T, I, K):
     c.close()
 
 
+@pytest.mark.parametrize("T, I, K", [(256, 2048, 128), (257, 2048, 384), (300, 2048, 128), (512, 2048, 640), (700, 2048, 128), (2100, 1408, 256),
+                                     (640, 896, 1152), (1000, 512, 128)])
+def test_tiles_of_many_tokens(T, I, K):
+    """On 32 compute units: tiles of 128 and of 256 tokens, one and several per workgroup, the last one with one token, some and all."""
+    c = S.Context(0)
+    c.set_partition(c.device_info()[0] - 32, 32)
+    rng = np.random.default_rng(I + T)
+    wg, wu = _weights(rng, I, K)
+    w = _pack(c, DEC, wg, wu)
+    x, b = _rows(rng, T, K)
+    got = _run(c, DEC, *mx_tensors(x, b), w, T, K, I)
+    pick = sorted({*range(0, T, 61), 127, 128, T - 2, T - 1})
+    _check(got[pick], x[pick], *(mx.quantise(v, mx.E2M1)[0] for v in (wg, wu)))
+    c.close()
+
+
 @pytest.mark.parametrize("T", [3, 20, 50, 100])
 @pytest.mark.parametrize("I", [128, 1408, 2048, 2560, 2816, 3584, 4096, 4224])
 def test_units_per_workgroup(T, I):
