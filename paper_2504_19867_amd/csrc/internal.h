@@ -404,8 +404,8 @@ hipError_t launch_ffn_gate_up(const void* x, const void* w_gu, void* out, int T,
 hipError_t launch_ffn_pack(const void* w_gate, const void* w_up, void* w_gu, int K, int I, hipStream_t stream);
 // Rows [T, hidden] bf16 (and the residual's, or null) normalised into out: bf16, or with out_scales E4M3 codes and scales [hidden / 128][T][4]
 constexpr int NORM_MOST_HIDDEN = 32768;
-hipError_t launch_rmsnorm(const void* x, void* residual, const void* weight, float eps, void* out, void* out_scales, int T, int hidden, int cus,
-                          const StepMark& mark, hipStream_t stream);
+hipError_t launch_rmsnorm(const void* x, void* residual, const void* weight, float eps, void* out, void* out_scales, int T, int hidden, const StepMark& mark,
+                          hipStream_t stream);
 // MXFP4 gate/up weights (w_mx: tiles of 128 outputs x 128 hidden entries, kernels_ffn_mx.hip), and their product with MX E4M3 rows x [T, K],
 // x_scales [K / 128][T][4]; K and I multiples of 128
 constexpr int FFN_MX_TILE_BYTES = 17 * 1024;

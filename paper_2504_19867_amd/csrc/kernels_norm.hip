@@ -6,9 +6,12 @@
 //
 // Bound by memory: every row is read once and written once.  A workgroup takes a row and keeps it in registers between the sum of squares
 // and the output; the block maxima of the 8-bit form are formed over the four lanes that hold a block.
+//
+// Two pieces of 8 entries per thread: one leaves half the loads on the way when the sum is waited for, four or more make few rows slow.  8-bit output with
+// the residual, by a phase of 128 compute units (7 bytes per entry; event times, which hold 4 us of launch): 8192 rows of hidden 4096, two / one / four pieces
+// 62.4 / 67.7 / 65.0 us (3.8 TB/s, where a copy reaches 4.3), 8192 rows of 8192 127 / 143 / 129, of 2048 25.0 / 27.6 / 24.8; one row of 8192
+// 6.0 / 6.0 / 7.1, of 16384 6.7 (1024 threads at most) and with four 6.8.
 #include "mx.h"
-
-#include <algorithm>
 
 namespace spd {
 
@@ -108,16 +111,16 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(NormArgs a) {
   }
 }
 
-hipError_t launch_rmsnorm(const void* x, void* residual, const void* weight, float eps, void* out, void* out_scales, int T, int hidden, int cus,
-                          const StepMark& mark, hipStream_t stream) {
-  (void)cus;
+hipError_t launch_rmsnorm(const void* x, void* residual, const void* weight, float eps, void* out, void* out_scales, int T, int hidden, const StepMark& mark,
+                          hipStream_t stream) {
   NormArgs a{(const bf16_t*)x, (bf16_t*)residual, (const bf16_t*)weight, out, (uint32_t*)out_scales, eps, T, hidden, mark};
   auto launch = [&](auto mx, auto bf, int threads) { hipLaunchKernelGGL(out_scales ? mx : bf, dim3((unsigned)T), dim3((unsigned)threads), 0, stream, a); };
   const int n = hidden / 8;
   if (n <= 64) launch(rmsnorm_kernel<64, 1, true>, rmsnorm_kernel<64, 1, false>, 64);
-  else if (n <= 256) launch(rmsnorm_kernel<256, 1, true>, rmsnorm_kernel<256, 1, false>, 256);
+  else if (n <= 128) launch(rmsnorm_kernel<64, 2, true>, rmsnorm_kernel<64, 2, false>, 64);
+  else if (n <= 256) launch(rmsnorm_kernel<128, 2, true>, rmsnorm_kernel<128, 2, false>, 128);
   else if (n <= 512) launch(rmsnorm_kernel<256, 2, true>, rmsnorm_kernel<256, 2, false>, 256);
-  else if (n <= 1024) launch(rmsnorm_kernel<256, 4, true>, rmsnorm_kernel<256, 4, false>, 256);
+  else if (n <= 1024) launch(rmsnorm_kernel<512, 2, true>, rmsnorm_kernel<512, 2, false>, 512);
   else if (n <= 2048) launch(rmsnorm_kernel<1024, 2, true>, rmsnorm_kernel<1024, 2, false>, 1024);
   else launch(rmsnorm_kernel<1024, 4, true>, rmsnorm_kernel<1024, 4, false>, 1024);
   return hipGetLastError();

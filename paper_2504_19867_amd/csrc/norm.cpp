@@ -16,13 +16,11 @@ extern "C" int spd_rmsnorm(spd_ctx* ctx, int phase, const void* x, void* residua
   if (residual && (residual == x || residual == out)) return SPD_EINVAL;   // it is read and written
   if (ctx->device < 0) return SPD_ESTATE;
   if (n_tokens == 0) return SPD_OK;
-  int share;
-  phase_exclusive(ctx, phase, &share);
   hipStream_t stream;
   int rc = phase_enter(ctx, phase, &stream);
   if (rc != SPD_OK) return rc;
   if ((rc = kernel_timing_mark(ctx, phase, 0, stream)) != SPD_OK) return rc;
-  SPD_HIP(launch_rmsnorm(x, residual, weight, eps, out, out_scales, n_tokens, hidden, share, step_mark(ctx, phase, stream_capturing(ctx, stream)),
+  SPD_HIP(launch_rmsnorm(x, residual, weight, eps, out, out_scales, n_tokens, hidden, step_mark(ctx, phase, stream_capturing(ctx, stream)),
                          stream));
   return kernel_timing_mark(ctx, phase, 1, stream);
 }
