@@ -13,6 +13,8 @@
 // 6.0 / 6.0 / 7.1, of 16384 6.7 (1024 threads at most) and with four 6.8.
 #include "mx.h"
 
+#include <algorithm>
+
 namespace spd {
 
 namespace {
@@ -33,16 +35,16 @@ struct NormArgs {
   void* out;
   uint32_t* scales;                                // [hidden / 128][T]: the four scale bytes of 128 entries
   float eps;
-  int T, hidden;
+  int T, hidden, first;                            // rows of all launches; this one's first
   StepMark mark;
 };
 }  // namespace
 
-// grid (T), block THREADS: a row of up to THREADS * PIECES pieces of 8 entries
+// grid (rows), block THREADS: a row of up to THREADS * PIECES pieces of 8 entries
 template <int THREADS, int PIECES, bool MX>
 __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(NormArgs a) {
   if (blockIdx.x == 0 && threadIdx.x == 0) store_mark(a.mark);
-  const int tid = threadIdx.x, n = a.hidden >> 3, t = blockIdx.x;
+  const int tid = threadIdx.x, n = a.hidden >> 3, t = a.first + blockIdx.x;
   const size_t row = (size_t)t * a.hidden;
   uint4 h[PIECES];
   float sum = 0.f;
@@ -113,8 +115,16 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(NormArgs a) {
 
 hipError_t launch_rmsnorm(const void* x, void* residual, const void* weight, float eps, void* out, void* out_scales, int T, int hidden, const StepMark& mark,
                           hipStream_t stream) {
-  NormArgs a{(const bf16_t*)x, (bf16_t*)residual, (const bf16_t*)weight, out, (uint32_t*)out_scales, eps, T, hidden, mark};
-  auto launch = [&](auto mx, auto bf, int threads) { hipLaunchKernelGGL(out_scales ? mx : bf, dim3((unsigned)T), dim3((unsigned)threads), 0, stream, a); };
+  NormArgs a{(const bf16_t*)x, (bf16_t*)residual, (const bf16_t*)weight, out, (uint32_t*)out_scales, eps, T, hidden, 0, mark};
+  constexpr int MOST_ROWS = 1 << 21;               // of a launch: a grid has fewer than 2^32 threads
+  auto launch = [&](auto mx, auto bf, int threads) {
+    for (a.first = 0; a.first < T; a.mark.flag = nullptr) {
+      const int rows = std::min(T - a.first, MOST_ROWS);
+      hipLaunchKernelGGL(out_scales ? mx : bf, dim3((unsigned)rows), dim3((unsigned)threads), 0, stream, a);
+      if (T - a.first <= MOST_ROWS) break;
+      a.first += MOST_ROWS;
+    }
+  };
   const int n = hidden / 8;
   if (n <= 64) launch(rmsnorm_kernel<64, 1, true>, rmsnorm_kernel<64, 1, false>, 64);
   else if (n <= 128) launch(rmsnorm_kernel<64, 2, true>, rmsnorm_kernel<64, 2, false>, 64);

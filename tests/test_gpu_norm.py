@@ -147,3 +147,32 @@ def test_captured_and_replayed(ctx):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, (out, codes, scales)))
     c.close()
+
+
+def test_more_rows_than_a_launch_takes(ctx):
+    """Short rows, more than 2^21 of them, and entries beyond 2^32: rows by the first and last launch."""
+    for T, hidden in ((2 ** 22 + 3, 8), (2 ** 21 + 1, 2056)):
+        gen = torch.Generator(device=DEV).manual_seed(hidden)
+        x = torch.empty(T, hidden, dtype=torch.bfloat16, device=DEV).normal_(generator=gen)
+        out, w = torch.zeros_like(x), torch.full((hidden,), 1.5, dtype=torch.bfloat16, device=DEV)
+        torch.cuda.synchronize()
+        ctx.rmsnorm(DEC, x, None, w, EPS, out, T, hidden)
+        ctx.phase_sync(DEC)
+        for rows in (slice(0, 5), slice(2 ** 21 - 2, 2 ** 21 + 2), slice(T - 5, T)):
+            h = x[rows].double().cpu().numpy()
+            y, _ = mx.rmsnorm(h, None, np.full(hidden, 1.5), EPS)
+            assert (np.abs(out[rows].double().cpu().numpy() - y) <= (2.0 ** -8 + DELTA) * np.abs(y)).all()
+
+
+def test_codes_beyond_4gib(ctx):
+    T, hidden = 2 ** 19 + 77, 8320
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.empty(T, hidden, dtype=torch.bfloat16, device=DEV).normal_(generator=gen)
+    w = torch.full((hidden,), 1.5, dtype=torch.bfloat16, device=DEV)
+    out, scales = torch.zeros(T, hidden, dtype=torch.uint8, device=DEV), torch.zeros(hidden // 128, T, 4, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    ctx.rmsnorm(DEC, x, None, w, EPS, out, T, hidden, out_scales=scales)
+    ctx.phase_sync(DEC)
+    for rows in (slice(0, 3), slice(T - 3, T)):
+        y, _ = mx.rmsnorm(x[rows].double().cpu().numpy(), None, np.full(hidden, 1.5), EPS)
+        assert_quantised(*mx_values(out[rows].contiguous(), scales[:, rows].contiguous(), 3, hidden), y, DELTA)

@@ -23,28 +23,35 @@ def test_norm(ctx):
     assert _norm(None) == S.SPD_EINVAL
     bad = [dict(phase=2), dict(phase=-1), dict(T=-1), dict(hidden=0), dict(hidden=-128), dict(hidden=200), dict(hidden=12, scales=None), dict(hidden=32896),
            dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(x=None), dict(w=None), dict(out=None),
-           dict(x=A + 8), dict(r=A + 8), dict(w=A + 8), dict(out=A + 8), dict(scales=A + 2), dict(r=A), dict(r=4 * A)]
+           dict(x=A + 8), dict(r=A + 8), dict(w=A + 8), dict(out=A + 8), dict(scales=A + 2), dict(r=A), dict(r=4 * A),
+           dict(out=A), dict(out=A + 2032, scales=None), dict(out=A - 16, scales=None), dict(r=A + 2032), dict(r=3 * A - 16), dict(out=2 * A + 16), dict(out=3 * A + 496),
+           dict(scales=A), dict(scales=2 * A + 2044), dict(scales=3 * A + 508), dict(scales=4 * A + 1020)]
     for b in bad:
         assert _norm(ctx, **b) == S.SPD_EINVAL, b
 
 
 def test_ffn(ctx):
-    def call(phase=1, x=A, xs=2 * A, w=3 * A, out=4 * A, T=4, hidden=256, inter=128):
+    def call(phase=1, x=A, xs=2 * A, w=32 * A, out=4 * A, T=4, hidden=256, inter=128):
         return S.lib.spd_ffn_gate_up_mx(ctx.h, phase, x, xs, w, out, T, hidden, inter)
-    assert call() == S.SPD_ESTATE and call(out=A + 2) == S.SPD_ESTATE and call(xs=A + 4) == S.SPD_ESTATE
+    assert call() == S.SPD_ESTATE and call(out=4 * A + 2) == S.SPD_ESTATE and call(xs=A + 4) == S.SPD_ESTATE
     assert S.lib.spd_ffn_gate_up_mx(None, 1, A, A, A, A, 4, 256, 128) == S.SPD_EINVAL
     for b in (dict(phase=2), dict(T=-1), dict(hidden=64), dict(hidden=0), dict(inter=64), dict(inter=-128), dict(hidden=1 << 24), dict(x=None), dict(xs=None),
-              dict(w=None), dict(out=None), dict(x=A + 8), dict(w=A + 8), dict(xs=A + 2), dict(out=A + 1)):
+              dict(w=None), dict(out=None), dict(x=A + 8), dict(w=A + 8), dict(xs=A + 2), dict(out=A + 1), dict(out=A), dict(out=A + 1022), dict(out=2 * A - 1022), dict(out=2 * A + 30),
+              dict(out=32 * A + 2 * 17408 - 2), dict(out=32 * A - 1022)):
         assert call(**b) == S.SPD_EINVAL, b
 
 
 def test_pack_and_unpack(ctx):
-    for fn in (S.lib.spd_ffn_pack_gate_up_mx, S.lib.spd_ffn_unpack_gate_up_mx):
-        assert fn(ctx.h, 0, A, A, A, 128, 128) == S.SPD_ESTATE
-        assert fn(None, 0, A, A, A, 128, 128) == S.SPD_EINVAL
-        for args in ((2, A, A, A, 128, 128), (0, None, A, A, 128, 128), (0, A, None, A, 128, 128), (0, A, A, None, 128, 128), (0, A + 8, A, A, 128, 128),
-                     (0, A, A + 8, A, 128, 128), (0, A, A, A + 8, 128, 128), (0, A, A, A, 96, 128), (0, A, A, A, 128, 192), (0, A, A, A, 0, 128)):
-            assert fn(ctx.h, *args) == S.SPD_EINVAL, args
+    gate, up, w = A, 32 * A, 64 * A                                              # 32768, 32768 and 17408 bytes
+    for fn, order in ((S.lib.spd_ffn_pack_gate_up_mx, (0, 1, 2)), (S.lib.spd_ffn_unpack_gate_up_mx, (2, 0, 1))):
+        def call(gate=gate, up=up, w=w, phase=0, hidden=128, inter=128, h=ctx.h):
+            at = (gate, up, w)
+            return fn(h, phase, *(at[i] for i in order), hidden, inter)
+        assert call() == S.SPD_ESTATE and call(up=gate + 32768) == S.SPD_ESTATE and call(w=up + 32768) == S.SPD_ESTATE
+        assert (call(up=gate) == S.SPD_ESTATE) == (order[0] == 0)                # both read, or both written
+        for b in (dict(h=None), dict(phase=2), dict(gate=None), dict(up=None), dict(w=None), dict(gate=A + 8), dict(up=A + 8), dict(w=A + 8), dict(hidden=96),
+                  dict(inter=192), dict(hidden=0), dict(w=gate + 32752), dict(w=up), dict(w=up - 17392)):
+            assert call(**b) == S.SPD_EINVAL, b
 
 
 def test_bytes():
