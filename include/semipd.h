@@ -96,7 +96,8 @@ int spd_device_info(spd_ctx* ctx, int* total_cus, int* xcds, int* cu_granularity
  * over those values.  Rows are written front to back: a write (spd_kv_write, a step's rows, an appended token) that begins at a
  * block's first position begins that block anew; one that begins further on keeps the block's rows ahead of it, under the larger of the block's
  * scale and the one that the new rows need (where it grows, rows ahead are rounded again); rows of the block behind the written ones are no
- * longer there.  A prefill step attends to its own rows as they are given (as on every pool) and to a cached prefix as it was cached before the
+ * longer there.  (So a block is neither read nor written by another call while a call writes rows into it, also where its rows ahead are
+ * long there: steps of one phase come one after the other, and a request is in one phase at a time.)  A prefill step attends to its own rows as they are given (as on every pool) and to a cached prefix as it was cached before the
  * step; with a prefix it brings all those rows together in library memory, 4 dim bytes per token and head, which the context keeps: SPD_ESTATE, and
  * nothing changes, where that memory cannot be had or the phase's stream is being captured into a graph.
  * The byte layout inside a page is private to the library (it is arranged for the
@@ -388,20 +389,21 @@ int spd_rmsnorm(spd_ctx* ctx, int phase, const void* x, void* residual, const vo
                 int32_t n_tokens, int32_t hidden);
 
 /* The gated FFN's first step (spd_ffn_gate_up) over weights in MXFP4 and rows in MXFP8: the same products and activation on the values that codes
- * and scales stand for, fp32 sums, one rounding to bf16 (nearest even).  17 / 32 byte per weight is read instead of 2.
+ * and scales stand for, fp32 sums of the matrix cores' sums of eight neighbouring entries' products, in which each product is cut to 2^-13 of the largest (so
+ * that where large ones cancel, that is how close), one rounding to bf16 (nearest even).  17 / 32 byte per weight is read instead of 2.
  * x device [n_tokens, hidden] E4M3 codes, x_scales device [hidden / 128][n_tokens][4] (as spd_rmsnorm writes them), w_mx device, of
  * spd_ffn_mx_bytes bytes, as spd_ffn_pack_gate_up_mx writes it (its order is private to the library), out device [n_tokens, inter] row-major,
  * bf16.  hidden and inter multiples of 128; x and w_mx 16-byte aligned, x_scales 4; n_tokens >= 0 (0: nothing is enqueued).  A NaN in a row
- * of x makes that row of out NaN, a block of weights that is NaN its column.  Enqueued on `phase`'s current stream; the buffers
+ * of x makes that row of out NaN, a block of weights that is NaN its column.  out overlaps nothing else.  Enqueued on `phase`'s current stream; the buffers
  * belong to the caller and must stay valid until the stream has run the call.  SPD_EINVAL on any violated condition, nothing enqueued. */
 int spd_ffn_gate_up_mx(spd_ctx* ctx, int phase, const void* x, const void* x_scales, const void* w_mx, void* out, int32_t n_tokens, int32_t hidden,
                        int32_t inter);
 /* Bytes of the packed weights: inter / 128 * hidden / 128 * 17408. */
 int spd_ffn_mx_bytes(int32_t hidden, int32_t inter, uint64_t* bytes_out);
 /* Quantises w_gate, w_up device [inter, hidden] row-major (bf16, 16-byte aligned) into w_mx (once per layer at load time).  A block of 32
- * hidden entries with an infinity or NaN becomes NaN as a whole (scale byte 255). */
+ * hidden entries with an infinity or NaN becomes NaN as a whole (scale byte 255).  w_mx overlaps neither. */
 int spd_ffn_pack_gate_up_mx(spd_ctx* ctx, int phase, const void* w_gate, const void* w_up, void* w_mx, int32_t hidden, int32_t inter);
-/* The values that w_mx stands for (exact in bf16), to w_gate, w_up.  For tests and for moving weights elsewhere. */
+/* The values that w_mx stands for (exact in bf16), to w_gate, w_up; none of the three overlaps another.  For tests and for moving weights elsewhere. */
 int spd_ffn_unpack_gate_up_mx(spd_ctx* ctx, int phase, const void* w_mx, void* w_gate, void* w_up, int32_t hidden, int32_t inter);
 
 /* A decode worker inside the library (paper, System Design, "Prefill and Decode Workers": the

@@ -75,7 +75,7 @@ class Cache8:
     def write(self, start: int, rows):
         rows = np.asarray(rows, dtype=np.float64)
         assert start <= len(self.rows)
-        at = 0
+        at, blocks, scales = 0, [], []
         while at < len(rows):
             blk, t = (start + at) // 16, (start + at) % 16
             n = min(16 - t, len(rows) - at)
@@ -86,6 +86,9 @@ class Cache8:
                 b = np.maximum(b, self.b[blk])
             s = np.exp2(b - 127.0)[None, :, None]
             block = nearest(np.concatenate([kept, new]) / s, E4M3) * s
-            self.rows = np.concatenate([self.rows[:blk * 16], block])
-            self.b = np.concatenate([self.b[:blk], b[None]])
+            blocks.append(block)
+            scales.append(b)
             at += n
+        if blocks:
+            self.rows = np.concatenate([self.rows[:start - start % 16], *blocks])
+            self.b = np.concatenate([self.b[:start // 16], np.stack(scales)])

@@ -418,6 +418,72 @@ def test_whole_prompts_are_what_a_bf16_pool_gives():
 
 
 # ----------------------------------------------------------------------------------------- large pools, graphs, both phases
+def test_a_waves_pages_change_windows():
+    """Chunks of more than 256 tiles, whose page numbers a wave holds in several goes; every number of steps behind the first 32, to the pipeline's depth."""
+    H, Hkv, D = 32, 32, 64
+    ctx = S.Context(0)
+    ctx.set_partition(ctx.device_info()[0] - 32, 32)
+    p = Pool8(Hkv, D, P=48, pages=900, ctx=ctx)
+    rng = np.random.default_rng(16)
+    lens = [4097, 4225, 4353, 4500, 8200, 9000]
+    for rid, n in enumerate(lens):
+        p.write(rid, 0, *_rows(rng, n - 1, Hkv, D))
+    for rid, n in enumerate(lens):
+        k, v = _rows(rng, 1, Hkv, D)
+        q = normal(rng, 1, H, D)
+        got = _decode(p, [rid], [n], q, D ** -0.5, k, v)
+        p.note(rid, n - 1, k, v)
+        _check_decode(p, [rid], [n], q, D ** -0.5, got)
+    p.close()
+    ctx.close()
+
+
+def test_rows_beyond_4gib():
+    """A prefix whose bf16 rows take more than 4 GiB for the keys: written, gathered, and attended to by a piece that begins inside a block."""
+    H, Hkv, D, n, m = 8, 8, 128, 2 ** 21 + 1003, 5
+    ctx = S.Context(0)
+    nbytes = S.pool_bytes(S.SPD_KV_GQA_FP8, 1024, Hkv, D, D, 2051)
+    mem = torch.full((nbytes,), 0xFF, dtype=torch.uint8, device=DEV)
+    pool = S.Pool(ctx, mem, nbytes, S.SPD_KV_GQA_FP8, 1024, Hkv, D, D, 2051)
+    gen = torch.Generator(device=DEV).manual_seed(17)
+    k, v = (torch.empty(n, Hkv, D, dtype=torch.bfloat16, device=DEV).normal_(generator=gen) for _ in range(2))
+    pool.kv_reserve(1, n)
+    torch.cuda.synchronize()
+    pool.kv_write(PRE, 1, 0, n, k, v)
+    ctx.phase_sync(PRE)
+    rows = [torch.zeros_like(k) for _ in range(2)]
+    torch.cuda.synchronize()
+    pool.kv_gather(PRE, 1, n, *rows)
+    ctx.phase_sync(PRE)
+    for got, given in zip(rows, (k, v)):
+        for begin, end in ((0, 40), (n - n % 16 - 32, n)):
+            cache = mx.Cache8(Hkv, D)
+            cache.write(0, given[begin:end].double().cpu().numpy())
+            np.testing.assert_array_equal(got[begin:end].double().cpu().numpy(), cache.rows)
+    del k, v
+    rng = np.random.default_rng(18)
+    q, kn, vn = normal(rng, m, H, D), *_rows(rng, m, Hkv, D)
+    tq, tk, tv = (bf16_tensor(t) for t in (q, kn, vn))
+    out = torch.zeros(m, H, D, dtype=torch.bfloat16, device=DEV)
+    torch.cuda.synchronize()
+    pool.prefill_step([1], [0, m], tq, tk, tv, out, H, Hkv, D, D, D ** -0.5, prefix_lens=[n])
+    ctx.phase_sync(PRE)
+    got = out.double().cpu().numpy()
+    hide = torch.arange(n + m, device=DEV)[None] > n + torch.arange(m, device=DEV)[:, None]
+    for h in range(H):                                   # `attention`, on the GPU
+        kk, vv = (torch.cat([r[:, h], t[:, h]]).double() for r, t in zip(rows, (tk, tv)))
+        qh = tq[:, h].double()
+        s = D ** -0.5 * qh @ kk.T.contiguous()
+        s[hide] = -torch.inf
+        weights = torch.softmax(s, -1)
+        mag = (D ** -0.5 * qh.abs() @ kk.abs().T.contiguous()).amax(-1, keepdim=True)
+        want, A = weights @ vv, weights @ vv.abs()
+        bar = (2.0 ** -7 + 2.0 ** -15 * mag) * A + 2.0 ** -8 * want.abs()
+        assert_close(got[:, h], (want.cpu().numpy(), bar.cpu().numpy()), f"head {h}")
+    pool.close()
+    ctx.close()
+
+
 def test_pages_beyond_4gib():
     Hkv, D, P = 8, 128, 16
     page_bytes = S.pool_bytes(S.SPD_KV_GQA_FP8, P, Hkv, D, D, 1)
@@ -477,7 +543,7 @@ def test_captured_and_replayed():
     with torch.cuda.graph(other, stream=pre):
         with pytest.raises(S.SpdError) as e:
             p.pool.prefill_step([1], [0, 4], rows, rows, rows, rows, 2, 2, 128, 128, 1.0, prefix_lens=[40])
-        p.ctx.rmsnorm(PRE, rows, None, rows, 1e-5, rows, 1, 256)                # (a graph wants a node)
+        p.ctx.rmsnorm(PRE, rows, None, q, 1e-5, rows, 1, 256)                   # (a graph wants a node)
     assert e.value.status == S.SPD_ESTATE
     assert ([p.pool.kv_block_table(r) for r in ids], p.pool.stats()) == tables
     torch.cuda.synchronize()
