@@ -46,73 +46,96 @@ typedef unsigned int u32x4_any __attribute__((ext_vector_type(4), aligned(2))); 
 // ---- the packed weights.  A tile is 128 outputs x 128 hidden entries; unit u of it (16 outputs) keeps, from byte 2048 u on, the codes of its
 // gate rows, then of its up rows, [quarter of 32 entries][row][16 bytes], and from byte 16384 + 128 u on the scales, [row][gate, up][quarter].
 // Four lanes per (row, quarter), eight entries each: 16 lanes have the 256 bytes of a row that lie in the tile.  Bound by memory: hidden 4096, inter
-// 14336 (235 MB of bf16, 62 MB packed) 64 us packed and 69 unpacked on 256 CUs (4.6 and 4.3 TB/s); with a lane per (row, quarter), whose 64 bytes of bf16 are four
-// accesses of its own, 80 and 97.
+// 14336 (235 MB of bf16, 62 MB packed) 54 us packed and 52 unpacked on 256 CUs (5.5 and 5.7 TB/s), 77 and 73 on 128 (4 TB/s), 132 and 134 on 64.  A workgroup has
+// four groups of 256 pieces on their way, and finds its tile once for all its threads; with one piece per thread, each dividing for itself, 62 and 80, 103 and
+// 119, 178 and 225.  With a lane per (row, quarter), whose 64 bytes of bf16 are four accesses of its own: 80 and 97 on 256 CUs.
 constexpr int SCALES_AT = 16384;
-struct PackPlace {
-  size_t tile;                                     // byte of the tile
-  size_t src;                                      // entry of the weight matrix
-  int up, quarter, row, unit, part;                // part: which eight of the quarter's 32 entries
-  __device__ PackPlace(long i, int n_kt, int hidden) {
-    const long t = i >> 12;
-    const int r = (int)(i & 4095);
-    part = r & 3; quarter = (r >> 2) & 3; row = (r >> 4) & 15; up = (r >> 8) & 1; unit = r >> 9;
-    const long tn = t / n_kt, kt = t % n_kt;
-    tile = (size_t)t * FFN_MX_TILE_BYTES;
-    src = (size_t)(tn * 128 + unit * 16 + row) * hidden + kt * 128 + quarter * 32 + part * 8;
+constexpr int PACK_GROUPS = 4;                     // groups whose loads a workgroup has on their way together: of one tile, which has 16
+// The 256 threads' place in a group: 16 rows of one side of a unit.  What differs from group to group is uniform.
+struct PackGroup {
+  size_t tile, src;                                // byte of the tile, first entry of the weight matrix
+  int up, unit;
+  __device__ PackGroup(uint32_t tile_no, int group, int n_kt, int hidden) {
+    const uint32_t tn = tile_no / (uint32_t)n_kt, kt = tile_no % (uint32_t)n_kt;
+    up = group & 1; unit = group >> 1;
+    tile = (size_t)tile_no * FFN_MX_TILE_BYTES;
+    src = (size_t)(tn * 128 + unit * 16) * hidden + kt * 128;
   }
-  __device__ size_t codes() const { return tile + unit * 2048 + up * 1024 + quarter * 256 + row * 16 + part * 4; }
-  __device__ size_t scale_word() const { return tile + SCALES_AT + unit * 128 + row * 8 + up * 4; }
+};
+struct PackLane {
+  int part, quarter, row;                          // part: which eight of the quarter's 32 entries
+  __device__ PackLane() : part(threadIdx.x & 3), quarter(threadIdx.x >> 2 & 3), row((int)threadIdx.x >> 4) {}
+  __device__ uint32_t src(int hidden) const { return (uint32_t)row * hidden + quarter * 32 + part * 8; }
+  __device__ uint32_t codes() const { return quarter * 256 + row * 16 + part * 4; }
+  __device__ uint32_t scales() const { return row * 8; }
 };
 
-// grid-stride over 4096 pieces per tile, block 256 (whole waves)
+// grid-stride over n_loads times PACK_GROUPS groups, block 256
 __global__ __launch_bounds__(256) void ffn_pack_mx_kernel(const bf16_t* __restrict__ wg, const bf16_t* __restrict__ wu, char* __restrict__ dst,
-                                                          int n_kt, int hidden, long n_pieces, StepMark mark) {
+                                                          int n_kt, int hidden, uint32_t n_loads, StepMark mark) {
   if (blockIdx.x == 0 && threadIdx.x == 0) store_mark(mark);
-  const long stride = (long)gridDim.x * blockDim.x;
-  for (long i = (long)blockIdx.x * blockDim.x + threadIdx.x; i < n_pieces; i += stride) {
-    const PackPlace p(i, n_kt, hidden);
-    const u32x4 w = __builtin_nontemporal_load((const u32x4*)((p.up ? wu : wg) + p.src));
-    uint32_t m = 0;
+  const PackLane lane;
+  for (uint32_t l = blockIdx.x; l < n_loads; l += gridDim.x) {
+    u32x4 in[PACK_GROUPS];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) m = max(m, max(w[j] << 16 & 0x7fffffff, w[j] & 0x7fff0000));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 1));   // (a quarter's four lanes)
-    m = max(m, (uint32_t)__shfl_xor((int)m, 2));
-    const bool finite = m < 0x7f800000;            // (E2M1 has neither infinities nor NaN: such a block is NaN as a whole)
-    const uint32_t b = finite ? scale_byte_e2m1(m) : MX_NAN_SCALE;
-    const float f = finite ? scale_of(b) : 1.f;
-    uint32_t c = 0;                                // (the conversion divides by the scale)
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, bf_lo(w[0]), bf_hi(w[0]), f, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, bf_lo(w[1]), bf_hi(w[1]), f, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, bf_lo(w[2]), bf_hi(w[2]), f, 2);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, bf_lo(w[3]), bf_hi(w[3]), f, 3);
-    *(uint32_t*)(dst + p.codes()) = c;
-    uint32_t four = b << (8 * p.quarter);          // the quarters of a row are 4 lanes apart
-    four |= (uint32_t)__shfl_xor((int)four, 4);
-    four |= (uint32_t)__shfl_xor((int)four, 8);
-    if (p.quarter == 0 && p.part == 0) *(uint32_t*)(dst + p.scale_word()) = four;
+    for (int g = 0; g < PACK_GROUPS; ++g) {
+      const PackGroup p(l / (16 / PACK_GROUPS), l % (16 / PACK_GROUPS) * PACK_GROUPS + g, n_kt, hidden);
+      in[g] = __builtin_nontemporal_load((const u32x4*)((p.up ? wu : wg) + p.src + lane.src(hidden)));
+    }
+#pragma unroll
+    for (int g = 0; g < PACK_GROUPS; ++g) {
+      const PackGroup p(l / (16 / PACK_GROUPS), l % (16 / PACK_GROUPS) * PACK_GROUPS + g, n_kt, hidden);
+      const u32x4 w = in[g];
+      uint32_t m = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) m = max(m, max(w[j] << 16 & 0x7fffffff, w[j] & 0x7fff0000));
+      m = max(m, (uint32_t)__shfl_xor((int)m, 1));   // (a quarter's four lanes)
+      m = max(m, (uint32_t)__shfl_xor((int)m, 2));
+      const bool finite = m < 0x7f800000;          // (E2M1 has neither infinities nor NaN: such a block is NaN as a whole)
+      const uint32_t b = finite ? scale_byte_e2m1(m) : MX_NAN_SCALE;
+      const float f = finite ? scale_of(b) : 1.f;
+      uint32_t c = 0;                              // (the conversion divides by the scale)
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, bf_lo(w[0]), bf_hi(w[0]), f, 0);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, bf_lo(w[1]), bf_hi(w[1]), f, 1);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, bf_lo(w[2]), bf_hi(w[2]), f, 2);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, bf_lo(w[3]), bf_hi(w[3]), f, 3);
+      *(uint32_t*)(dst + p.tile + p.unit * 2048 + p.up * 1024 + lane.codes()) = c;
+      uint32_t four = b << (8 * lane.quarter);     // the quarters of a row are 4 lanes apart
+      four |= (uint32_t)__shfl_xor((int)four, 4);
+      four |= (uint32_t)__shfl_xor((int)four, 8);
+      if (lane.quarter == 0 && lane.part == 0) *(uint32_t*)(dst + p.tile + SCALES_AT + p.unit * 128 + p.up * 4 + lane.scales()) = four;
+    }
   }
 }
 
 // The values that the packed weights stand for (exact in bf16).
 __global__ __launch_bounds__(256) void ffn_unpack_mx_kernel(const char* __restrict__ w, bf16_t* __restrict__ wg, bf16_t* __restrict__ wu, int n_kt,
-                                                            int hidden, long n_pieces, StepMark mark) {
+                                                            int hidden, uint32_t n_loads, StepMark mark) {
   if (blockIdx.x == 0 && threadIdx.x == 0) store_mark(mark);
-  const long stride = (long)gridDim.x * blockDim.x;
-  for (long i = (long)blockIdx.x * blockDim.x + threadIdx.x; i < n_pieces; i += stride) {
-    const PackPlace p(i, n_kt, hidden);
-    const uint32_t c = *(const uint32_t*)(w + p.codes());
-    const uint32_t b = *(const uint8_t*)(w + p.scale_word() + p.quarter);
-    const float f = b == MX_NAN_SCALE ? __builtin_nanf("") : scale_of(b);
-    auto value = [&](uint32_t code) -> float {
-      const uint32_t e = code >> 1 & 3, man = code & 1;
-      const float v = e ? __builtin_bit_cast(float, (e + 126) << 23 | man << 22) : 0.5f * (float)man;
-      return (code & 8 ? -v : v) * f;
-    };
-    u32x4 o;
+  const PackLane lane;
+  for (uint32_t l = blockIdx.x; l < n_loads; l += gridDim.x) {
+    uint32_t codes[PACK_GROUPS], scales[PACK_GROUPS];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = pack_bf16(value(c >> (8 * e) & 15), value(c >> (8 * e + 4) & 15));
-    __builtin_nontemporal_store(o, (u32x4*)((p.up ? wu : wg) + p.src));
+    for (int g = 0; g < PACK_GROUPS; ++g) {
+      const PackGroup p(l / (16 / PACK_GROUPS), l % (16 / PACK_GROUPS) * PACK_GROUPS + g, n_kt, hidden);
+      codes[g] = *(const uint32_t*)(w + p.tile + p.unit * 2048 + p.up * 1024 + lane.codes());
+      scales[g] = *(const uint8_t*)(w + p.tile + SCALES_AT + p.unit * 128 + p.up * 4 + lane.scales() + lane.quarter);
+    }
+#pragma unroll
+    for (int g = 0; g < PACK_GROUPS; ++g) {
+      const PackGroup p(l / (16 / PACK_GROUPS), l % (16 / PACK_GROUPS) * PACK_GROUPS + g, n_kt, hidden);
+      const uint32_t c = codes[g];
+      const float f = scales[g] == MX_NAN_SCALE ? __builtin_nanf("") : scale_of(scales[g]);
+      auto value = [&](uint32_t code) -> float {
+        const uint32_t e = code >> 1 & 3, man = code & 1;
+        const float v = e ? __builtin_bit_cast(float, (e + 126) << 23 | man << 22) : 0.5f * (float)man;
+        return (code & 8 ? -v : v) * f;
+      };
+      u32x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = pack_bf16(value(c >> (8 * e) & 15), value(c >> (8 * e + 4) & 15));
+      __builtin_nontemporal_store(o, (u32x4*)((p.up ? wu : wg) + p.src + lane.src(hidden)));
+    }
   }
 }
 
@@ -532,19 +555,18 @@ hipError_t launch_ffn_gate_up_mx(const void* x, const void* x_scales, const void
   return launch_mx_stream<8>(x, x_scales, w_mx, out, T, K, I, cus, mark, stream);
 }
 
-static unsigned pack_grid(long n_pieces) { return (unsigned)std::min<long>((n_pieces + 255) / 256, 8192); }
+// pack and unpack: rounds of PACK_GROUPS groups (a matrix pair that fits the card has fewer than 2^32), and workgroups
+static uint32_t pack_loads(int K, int I) { return (uint32_t)((int64_t)(I / 128) * (K / 128) * (16 / PACK_GROUPS)); }
 
 hipError_t launch_ffn_pack_mx(const void* w_gate, const void* w_up, void* w_mx, int K, int I, const StepMark& mark, hipStream_t stream) {
-  const long n_pieces = (long)(I / 128) * (K / 128) * 4096;
-  hipLaunchKernelGGL(ffn_pack_mx_kernel, dim3(pack_grid(n_pieces)), dim3(256), 0, stream, (const bf16_t*)w_gate, (const bf16_t*)w_up, (char*)w_mx, K / 128,
-                     K, n_pieces, mark);
+  const uint32_t n = pack_loads(K, I);
+  hipLaunchKernelGGL(ffn_pack_mx_kernel, dim3(std::min(n, 8192u)), dim3(256), 0, stream, (const bf16_t*)w_gate, (const bf16_t*)w_up, (char*)w_mx, K / 128, K, n, mark);
   return hipGetLastError();
 }
 
 hipError_t launch_ffn_unpack_mx(const void* w_mx, void* w_gate, void* w_up, int K, int I, const StepMark& mark, hipStream_t stream) {
-  const long n_pieces = (long)(I / 128) * (K / 128) * 4096;
-  hipLaunchKernelGGL(ffn_unpack_mx_kernel, dim3(pack_grid(n_pieces)), dim3(256), 0, stream, (const char*)w_mx, (bf16_t*)w_gate, (bf16_t*)w_up, K / 128, K,
-                     n_pieces, mark);
+  const uint32_t n = pack_loads(K, I);
+  hipLaunchKernelGGL(ffn_unpack_mx_kernel, dim3(std::min(n, 8192u)), dim3(256), 0, stream, (const char*)w_mx, (bf16_t*)w_gate, (bf16_t*)w_up, K / 128, K, n, mark);
   return hipGetLastError();
 }
 
