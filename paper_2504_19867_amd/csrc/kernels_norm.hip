@@ -81,7 +81,13 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(NormArgs a) {
 #pragma unroll
     for (int i = 0; i < THREADS / 64; ++i) sum += part[i];
   }
-  const float inv = 1.f / sqrtf(sum / (float)a.hidden + a.eps);
+  // (a scale byte turns on whether a block's largest y passes a border: the root, its inverse and the products are carried to half a step of fp32)
+  const float mean = sum / (float)a.hidden + a.eps, r0 = 1.f / sqrtf(mean), mr = mean * r0;
+  const float inv = !(r0 > 0.f) ? r0 : __builtin_fmaf(0.5f * r0, __builtin_fmaf(-mr, r0, 1.f) - __builtin_fmaf(mean, r0, -mr) * r0, r0);
+  auto product = [&](float hv, float wv) -> float {
+    const float y = hv * inv;
+    return __builtin_isfinite(y) ? __builtin_fmaf(y, wv, __builtin_fmaf(hv, inv, -y) * wv) : y * wv;
+  };
 #pragma unroll
   for (int j = 0; j < PIECES; ++j) {
     const int p = tid + THREADS * j;
@@ -91,8 +97,8 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(NormArgs a) {
     float y[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      y[2 * i] = bf_lo(hw[i]) * inv * bf_lo(ww[i]);
-      y[2 * i + 1] = bf_hi(hw[i]) * inv * bf_hi(ww[i]);
+      y[2 * i] = product(bf_lo(hw[i]), bf_lo(ww[i]));
+      y[2 * i + 1] = product(bf_hi(hw[i]), bf_hi(ww[i]));
     }
     if constexpr (!MX) {
       *(uint4*)((bf16_t*)a.out + row + 8 * p) = uint4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
