@@ -85,8 +85,8 @@ __global__ __launch_bounds__(THREADS) void rmsnorm_kernel(NormArgs a) {
   const float mean = sum / (float)a.hidden + a.eps, r0 = 1.f / sqrtf(mean), mr = mean * r0;
   const float inv = !(r0 > 0.f) ? r0 : __builtin_fmaf(0.5f * r0, __builtin_fmaf(-mr, r0, 1.f) - __builtin_fmaf(mean, r0, -mr) * r0, r0);
   auto product = [&](float hv, float wv) -> float {
-    const float y = hv * inv;
-    return __builtin_isfinite(y) ? __builtin_fmaf(y, wv, __builtin_fmaf(hv, inv, -y) * wv) : y * wv;
+    const float y = hv * inv, p = y * wv;
+    return __builtin_isfinite(p) ? __builtin_fmaf(y, wv, __builtin_fmaf(hv, inv, -y) * wv) : p;
   };
 #pragma unroll
   for (int j = 0; j < PIECES; ++j) {

@@ -108,6 +108,38 @@ def test_what_is_not_finite_stays_in_its_row(ctx):
         assert (np.isnan(o[1]).all() if np.isnan(bad) else (np.delete(o[1], 77) == 0).all())
 
 
+@pytest.mark.parametrize("mx8", [False, True])
+def test_weights_that_are_not_finite_stay_in_their_column(ctx, mx8):
+    """h w / rms as it is: infinite by the signs of h and w, NaN where h is 0; in 8 bits NaN, and the other entries of the block as if it were not there."""
+    rng = np.random.default_rng(13)
+    T, hidden = 40, 256
+    x, w = normal(rng, T, hidden), normal(rng, hidden)
+    bad = {5: np.inf, 40: -np.inf, 41: np.inf, 100: np.nan, 255: -np.inf}
+    x[3, 5] = x[7, 255] = 0
+    clean = w.copy()
+    clean[list(bad)] = 0
+    for col, value in bad.items():
+        w[col] = value
+    tx, tw = bf16_tensor(x), bf16_tensor(w)
+    out, scales = _bytes(T, hidden) if mx8 else (torch.zeros(T, hidden, dtype=torch.bfloat16, device=DEV), None)
+    torch.cuda.synchronize()
+    ctx.rmsnorm(DEC, tx, None, tw, EPS, out, T, hidden, out_scales=scales)
+    ctx.phase_sync(DEC)
+    with np.errstate(invalid="ignore"):
+        lost = x[:, list(bad)] * w[list(bad)]            # (the root is finite and positive)
+    y, _ = mx.rmsnorm(x, None, clean, EPS)
+    if mx8:
+        got, b = mx_values(out[:T * hidden], scales[:T * hidden // 32], T, hidden)
+        assert np.isnan(got[:, list(bad)]).all()
+        got[:, list(bad)] = 0
+        assert_quantised(got, b, y, DELTA)
+    else:
+        got = out.double().cpu().numpy()
+        np.testing.assert_array_equal(got[:, list(bad)], lost)
+        got[:, list(bad)] = 0
+        assert (np.abs(got - y) <= (2.0 ** -8 + DELTA) * np.abs(y)).all()
+
+
 def test_in_place_and_without_rows(ctx):
     rng = np.random.default_rng(11)
     x, w = normal(rng, 9, 1032), normal(rng, 1032)
