@@ -378,7 +378,7 @@ int spd_ffn_pack_gate_up(spd_ctx* ctx, int phase, const void* w_gate, const void
 
 /* RMS norm, with the addition of the residual stream ahead of it (the step ahead of either half of a layer of the Llama models):
  *     h = bf16(x + residual), residual <- h (residual NULL: h = x),     y_i = h_i weight_i / sqrt(mean_j h_j^2 + eps)
- * sums and products in fp32 (entries of a magnitude whose squares pass fp32's range are not meant).
+ * the sum of squares in fp64, y rounded once to fp32 ahead of the output's rounding.
  * x, residual device [n_tokens, hidden], weight device [hidden], bf16.  With out_scales NULL, out is device [n_tokens, hidden] bf16 (nearest
  * even) and hidden a multiple of 8.  Else out is device [n_tokens, hidden] bytes, the E4M3 codes of y (infinities and NaN: NaN), and out_scales
  * device [hidden / 128][n_tokens][4] bytes, the scale of entries 128 a + 32 b .. + 31 of row t at [a][t][b]: the form that

@@ -140,6 +140,71 @@ def test_weights_that_are_not_finite_stay_in_their_column(ctx, mx8):
         assert (np.abs(got - y) <= (2.0 ** -8 + DELTA) * np.abs(y)).all()
 
 
+@pytest.mark.parametrize("mx8", [False, True])
+@pytest.mark.parametrize("seed", [0, 1, 2])
+def test_sums_whose_last_bits_decide(ctx, seed, mx8):
+    """One large entry and thousands whose squares a sum in 24 bits next to it would round.  eps makes the root 64, so that y = h w / 64 is exact and many
+    entries lie halfway between two codes (or bf16 values): all go to the even one."""
+    rng = np.random.default_rng(seed)
+    hidden = 4096
+    x = rng.integers(112, 128, (1, hidden)) / 16 * rng.choice([-1.0, 1.0], (1, hidden))
+    x[0, rng.integers(hidden)] = 4064
+    eps = 4096 - (x * x).mean()
+    assert eps > 0 and eps == np.float32(eps)
+    for w in (np.full(hidden, 64.0), rng.integers(128, 256, hidden) / 4):
+        y, _ = mx.rmsnorm(x, None, w, eps)
+        assert np.array_equal(y, x * w / 64)
+        tx, tw = bf16_tensor(x), bf16_tensor(w)
+        out, scales = _bytes(1, hidden) if mx8 else (torch.zeros(1, hidden, dtype=torch.bfloat16, device=DEV), None)
+        torch.cuda.synchronize()
+        ctx.rmsnorm(PRE, tx, None, tw, eps, out, 1, hidden, out_scales=scales)
+        ctx.phase_sync(PRE)
+        if mx8:
+            got, b = mx_values(out[:hidden], scales[:hidden // 32], 1, hidden)
+            want, wb = mx.quantise(y, mx.E4M3)
+            assert np.array_equal(b, wb) and np.array_equal(got, want), (got != want).sum()
+        else:
+            got, want = out.double().cpu().numpy(), mx.to_bf16(y)
+            assert np.array_equal(got, want), (got != want).sum()
+
+
+def test_codes_of_y_rounded_to_fp32(ctx):
+    """The 8-bit form's y is off by one rounding to fp32 (2^-24) and next to nothing else, whatever the row's length."""
+    rng = np.random.default_rng(14)
+    for T, hidden in ((400, 4096), (60, 16384), (700, 384)):
+        x, r, w = normal(rng, T, hidden, spread=6), normal(rng, T, hidden, spread=6), normal(rng, hidden)
+        tx, tr, tw = bf16_tensor(x), bf16_tensor(r), bf16_tensor(w)
+        out, scales = _bytes(T, hidden)
+        torch.cuda.synchronize()
+        ctx.rmsnorm(PRE, tx, tr, tw, EPS, out, T, hidden, out_scales=scales)
+        ctx.phase_sync(PRE)
+        got, b = mx_values(out[:T * hidden], scales[:T * hidden // 32], T, hidden)
+        assert_quantised(got, b, mx.rmsnorm(x, r, w, float(np.float32(EPS)))[0], 2.0 ** -24 + 2.0 ** -38)
+
+
+@pytest.mark.parametrize("mx8", [False, True])
+def test_magnitudes_whose_squares_pass_fp32(ctx, mx8):
+    rng = np.random.default_rng(15)
+    x, w = normal(rng, 4, 512), normal(rng, 512)
+    x *= np.array([2.0 ** 70, 2.0 ** 120, 2.0 ** -90, 2.0 ** 63])[:, None]
+    got = _run(ctx, DEC, x, None, w, mx8)
+    assert (got[[0, 1, 3]].any(1)).all()
+    assert (_run(ctx, DEC, x[2:3], None, w, mx8, eps=2.0 ** -148) != 0).any()         # below fp32's range
+
+
+def test_a_row_of_infinite_root(ctx):
+    """Whatever is finite in it weighs nothing, also where entry times weight passes fp32's range."""
+    x, w = np.zeros((1, 128)), np.ones(128)
+    x[0, 3], x[0, 9], w[9], x[0, 20] = np.inf, 2.0 ** 127, 2.0 ** 100, 5
+    tx, tw = bf16_tensor(x), bf16_tensor(w)
+    out = torch.empty_like(tx)
+    torch.cuda.synchronize()
+    ctx.rmsnorm(DEC, tx, None, tw, EPS, out, 1, 128)
+    ctx.phase_sync(DEC)
+    o = out.double().cpu().numpy()[0]
+    assert np.isnan(o[3]) and (np.delete(o, 3) == 0).all()
+
+
 def test_in_place_and_without_rows(ctx):
     rng = np.random.default_rng(11)
     x, w = normal(rng, 9, 1032), normal(rng, 1032)
