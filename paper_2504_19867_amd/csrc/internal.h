@@ -374,7 +374,7 @@ hipError_t launch_kv_write_fp8(const PoolGeom& g, char* pool_base, const TileDes
                                uint64_t copy_bytes = 0);
 hipError_t launch_kv_gather_fp8(const PoolGeom& g, const char* pool_base, const TileDesc* d_tiles, int n_tiles, void* out,
                                 const StepMark& mark, hipStream_t stream);
-// GQA pools in 8 bits (kernels_kv_gqa_fp8.hip): everything that KvRows says but the rotation; launch_kv_rows and launch_kv_gather lead there.
+// GQA pools in 8 bits (kernels_kv_gqa_fp8.hip): everything that KvRows says but the rotation; launch_kv_rows leads there.
 // A block that d_tiles writes from its middle on must not be among d_cached: with k_all its earlier rows go there too, ahead of TileDesc.pad[1].
 hipError_t launch_kv_rows_gqa_fp8(const PoolGeom& g, char* pool_base, const TileDesc* d_tiles, int n_tiles, const void* k, const void* v,
                                   const KvRows& x, const StepMark& mark, hipStream_t stream);

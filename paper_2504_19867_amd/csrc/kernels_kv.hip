@@ -656,12 +656,6 @@ hipError_t launch_kv_write(const PoolGeom& g, char* pool_base, const TileDesc* d
 hipError_t launch_kv_gather(const PoolGeom& g, const char* pool_base, const TileDesc* d_tiles, int n_tiles, void* k_out,
                             void* v_out, const StepMark& mark, hipStream_t stream) {
   if (n_tiles <= 0) return hipSuccess;
-  if (g.kind == SPD_KV_GQA_FP8) {
-    KvRows x;
-    x.d_cached = d_tiles; x.n_cached = n_tiles;
-    x.k_all = k_out; x.v_all = v_out;
-    return launch_kv_rows_gqa_fp8(g, (char*)pool_base, nullptr, 0, nullptr, nullptr, x, mark, stream);
-  }
   hipLaunchKernelGGL(kv_gather_kernel, dim3(n_tiles, g.Hkv), dim3(256), 0, stream, pool_base, g.page_bytes,
                      g.head_bytes, g.tile_bytes, g.tile_k_bytes, d_tiles, (bf16_t*)k_out, (bf16_t*)v_out, g.Hkv, g.dk,
                      g.dv, g.kind == SPD_KV_MLA_LATENT ? 1 : 0, mark);

@@ -224,7 +224,10 @@ __global__ __launch_bounds__(256, 4) void kv_write_gqa_fp8_kernel(Rows8Args a) {
 }
 
 // KV heads per workgroup: one per wave, unless there are so many tiles that workgroups queue for compute units; then the reads of the descriptors, which
-// may lie in pinned host memory, are worth halving.
+// may lie in pinned host memory, are worth halving.  Rows read back, in us with two heads per wave / one: 16 of 8 heads 5.4 / 4.8 on 128 CUs, 1000 6.0 / 5.6,
+// 3000 7.8 / 7.1; of 32 heads on 256 CUs 250 6.4 / 5.1, 2000 12.5 / 11.3, on 128 CUs 1000 9.3 / 8.2.  The read, whose workgroups wait for little else than
+// descriptors, stops at 200 tiles: 3500 rows of 8 heads 8.2 / 8.7 on 128 CUs, 7.6 / 8.2 on 256, 4000 8.7 / 9.4 and 8.0 / 8.6 (the write 9.8 / 9.6).
+constexpr int MOST_TILES_READ_BY_HEAD = 200;
 static int heads_per_workgroup(int n_tiles, int Hkv, int cus) { return (int64_t)n_tiles * ((Hkv + 3) / 4) <= 4 * (int64_t)cus ? 4 : 8; }
 
 hipError_t launch_kv_rows_gqa_fp8(const PoolGeom& g, char* pool_base, const TileDesc* d_tiles, int n_tiles, const void* k, const void* v,
@@ -240,9 +243,9 @@ hipError_t launch_kv_rows_gqa_fp8(const PoolGeom& g, char* pool_base, const Tile
   a.n_copy = (int)std::min<uint64_t>(128, (a.copy_n16 + 255) / 256);
   a.k_all = (bf16_t*)x.k_all; a.v_all = (bf16_t*)x.v_all;
   a.mark = mark;
-  // what is done to `tiles` tiles, `copying` workgroups ahead of them
-  auto launch = [&](auto kernel, int tiles, int copying) -> hipError_t {
-    a.HG = heads_per_workgroup(tiles, g.Hkv, x.cus); a.groups = (g.Hkv + a.HG - 1) / a.HG;
+  // what is done to `tiles` tiles, `heads` KV heads per workgroup, `copying` workgroups ahead of them
+  auto launch = [&](auto kernel, int tiles, int copying, int heads) -> hipError_t {
+    a.HG = heads; a.groups = (g.Hkv + a.HG - 1) / a.HG;
     const int64_t blocks = copying + (int64_t)tiles * a.groups;
     if (blocks <= 0) return hipSuccess;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
@@ -251,12 +254,14 @@ hipError_t launch_kv_rows_gqa_fp8(const PoolGeom& g, char* pool_base, const Tile
     return hipGetLastError();
   };
   a.descs = d_tiles;
+  int heads = heads_per_workgroup(n_tiles, g.Hkv, x.cus);
   hipError_t e;
-  if (g.dk == 128) e = launch(kv_write_gqa_fp8_kernel<128>, n_tiles, a.n_copy);
-  else e = launch(kv_write_gqa_fp8_kernel<64>, n_tiles, a.n_copy);
+  if (g.dk == 128) e = launch(kv_write_gqa_fp8_kernel<128>, n_tiles, a.n_copy, heads);
+  else e = launch(kv_write_gqa_fp8_kernel<64>, n_tiles, a.n_copy, heads);
   if (e != hipSuccess) return e;
   a.descs = x.d_cached;
-  return g.dk == 128 ? launch(kv_read_gqa_fp8_kernel<128>, x.n_cached, 0) : launch(kv_read_gqa_fp8_kernel<64>, x.n_cached, 0);
+  heads = x.n_cached > MOST_TILES_READ_BY_HEAD ? 8 : heads_per_workgroup(x.n_cached, g.Hkv, x.cus);
+  return g.dk == 128 ? launch(kv_read_gqa_fp8_kernel<128>, x.n_cached, 0, heads) : launch(kv_read_gqa_fp8_kernel<64>, x.n_cached, 0, heads);
 }
 
 }  // namespace spd

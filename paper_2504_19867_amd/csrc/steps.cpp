@@ -116,7 +116,11 @@ static int kv_copy(spd_ctx* ctx, spd_pool* pool, int phase, uint64_t req_id, int
   const bool fp8 = g.kind == SPD_KV_MLA_LATENT_FP8;
   KvRows rows;
   phase_exclusive(ctx, phase, &rows.cus);                         // (its share)
-  if (write && fp8) SPD_HIP(launch_kv_write_fp8(g, pool->base, descs, n_descs, k, mark, stream));
+  if (!write && g.kind == SPD_KV_GQA_FP8) {                       // a gather is a rows launch that has only cached rows
+    rows.d_cached = descs; rows.n_cached = n_descs;
+    rows.k_all = (void*)k; rows.v_all = (void*)v;
+    SPD_HIP(launch_kv_rows(g, pool->base, nullptr, 0, nullptr, nullptr, rows, mark, stream));
+  } else if (write && fp8) SPD_HIP(launch_kv_write_fp8(g, pool->base, descs, n_descs, k, mark, stream));
   else if (write && kv_rows_supported(g)) SPD_HIP(launch_kv_rows(g, pool->base, descs, n_descs, k, v, rows, mark, stream));
   else if (write) SPD_HIP(launch_kv_write(g, pool->base, descs, n_descs, k, v, mark, stream));
   else if (fp8) SPD_HIP(launch_kv_gather_fp8(g, pool->base, descs, n_descs, (void*)k, mark, stream));
