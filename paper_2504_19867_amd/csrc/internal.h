@@ -402,9 +402,9 @@ hipError_t launch_prefill(const void* q, const void* k, const void* v, void* out
 hipError_t launch_ffn_gate_up(const void* x, const void* w_gu, void* out, int T, int K, int I, int xcds, int cus, bool exclusive,
                               const StepMark& mark, hipStream_t stream);
 hipError_t launch_ffn_pack(const void* w_gate, const void* w_up, void* w_gu, int K, int I, hipStream_t stream);
-// do `na` bytes from a on and `nb` from b on share one (null: no)
+// do `na` bytes from a on and `nb` from b on share one (null, or no bytes: no)
 inline bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
-  return a && b && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+  return a && b && na && nb && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
 // Rows [T, hidden] bf16 (and the residual's, or null) normalised into out: bf16, or with out_scales E4M3 codes and scales [hidden / 128][T][4]
 constexpr int NORM_MOST_HIDDEN = 32768;

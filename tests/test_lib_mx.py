@@ -60,3 +60,10 @@ def test_bytes():
         with pytest.raises(S.SpdError):
             S.ffn_mx_bytes(hidden, inter)
     assert S.lib.spd_ffn_mx_bytes(128, 128, None) == S.SPD_EINVAL
+
+
+def test_no_rows_overlap_nothing(ctx):
+    """Without tokens an output of no bytes may point anywhere, into the weights too."""
+    assert S.lib.spd_rmsnorm(ctx.h, 1, A, None, 3 * A, 1e-5, 3 * A + 16, None, 0, 256) == S.SPD_ESTATE
+    assert S.lib.spd_rmsnorm(ctx.h, 1, A, 3 * A + 32, 3 * A, 1e-5, 4 * A, 3 * A + 16, 0, 256) == S.SPD_ESTATE
+    assert S.lib.spd_ffn_gate_up_mx(ctx.h, 1, A, A, 2 * A, 2 * A + 16, 0, 256, 128) == S.SPD_ESTATE
