@@ -417,6 +417,27 @@ def test_whole_prompts_are_what_a_bf16_pool_gives():
     assert all(torch.equal(a, b) for a, b in zip(*outs))
 
 
+@pytest.mark.parametrize("Hkv, D", [(8, 128), (9, 64)])
+def test_two_heads_per_wave_and_a_piece_that_begins_inside_a_block(Hkv, D):
+    """More tiles than a small share has workgroups for, so that a wave takes two heads in turn: rows ahead of the piece are re-coded and, behind a
+    cached prefix, handed out by both."""
+    ctx = S.Context(0)
+    total = ctx.device_info()[0]
+    p = Pool8(Hkv, D, pages=400, ctx=ctx)
+    rng = np.random.default_rng(Hkv)
+    ctx.set_partition(total - 32, 32)
+    for rid, kept, grow in ((1, 7, 2.0 ** 6), (2, 15, 2.0 ** -9), (3, 1, 2.0 ** 40)):
+        p.write(rid, 0, *_rows(rng, kept, Hkv, D))
+        p.write(rid, kept, *(r * grow for r in _rows(rng, 1100, Hkv, D)))
+        p.assert_rows(rid)
+    ctx.set_partition(32, total - 32)
+    _prefill(p, [4, 5], [39, 30], None, Hkv, rng)
+    _prefill(p, [4, 5], [1100, 70], [39, 30], Hkv, rng, spread=4)
+    _prefill(p, [4], [1050], [1139], Hkv, rng, S.rope_config(rotary_dim=D))
+    p.close()
+    ctx.close()
+
+
 # ----------------------------------------------------------------------------------------- large pools, graphs, both phases
 def test_a_waves_pages_change_windows():
     """Chunks of more than 256 tiles, whose page numbers a wave holds in several goes; every number of steps behind the first 32, to the pipeline's depth."""
