@@ -372,17 +372,24 @@ extern "C" int spd_prefill_step(spd_ctx* ctx, spd_pool* pool, const spd_prefill_
 }
 
 // ------------------------------------------------------------------------------------------ decode
-// A compute unit holds two workgroups of the GQA kernel (64-dim heads: three).  From the third (fifth) on, what each of them does
+// A compute unit holds two workgroups of the GQA kernel (64-dim heads, and pages in 8 bits: three).  From the third (fifth) on, what each of them does
 // before its first tile is waited for in turn.
 // Then the records are copied to the device first: with 30-token contexts on 64 .. 256 CUs reading them there takes 0.81 .. 0.98 of
 // the step's time with the reads over the host link, 3 to 24 workgroups per compute unit; 1.02 .. 1.15 below 3.
-static bool gqa_many(int n_wgs, int share, int dim) { return dim > 64 ? n_wgs >= 3 * share : n_wgs > 4 * share; }
+// Pages in 8 bits, 128 dims, append without rotation / with it, in one launch | with the two ahead of it: 3 workgroups per compute unit, 30 .. 60 tokens
+// 9.0 / 11.5 | 12.1 / 12.9 us on 128 CUs, 9.5 / 12.0 | 13.4 / 14.3 on 256; 4, 500 .. 1000 tokens 29.7 / 32.7 | 31.0 / 32.3; 6, 30 .. 60 tokens
+// 16.3 / 21.0 | 16.4 / 17.9; 12.5 34.8 / 45.2 | 26.7 / 28.7.
+static bool gqa_many(int n_wgs, int share, int dim, bool eight) { return dim > 64 && !eight ? n_wgs >= 3 * share : n_wgs > 4 * share; }
 // And where HBM does not hide it, a launch rotates and appends for all of them.  It does where the workgroups' rows, at the rate
 // of all the share's compute units, take longer: line at 32 MiB (no rotation: 24) of mean bytes per workgroup times compute units.
 // Step without the launch ahead / with it, 8 KV heads of 128 dims with RoPE, tokens per workgroup: 64 CUs 200 1.35 .. 1.51,
 // 590 1.12, 1000 1.05, 1729 1.01; 128 CUs 200 1.23, 365 1.09, 600 1.02, 914 0.99; 256 CUs 164 1.03 .. 1.05, 274 0.99, 579 0.96.  Append
 // alone: 64 CUs 590 1.03, 914 0.99; 128 CUs 300 1.00 .. 1.02, 450 0.96; 256 CUs 200 0.99.
 static bool gqa_prepares(int64_t bytes, int n_wgs, int share, bool rope) { return bytes / n_wgs * share <= (rope ? 32 << 20 : 24 << 20); }
+// Pages in 8 bits: the line is in tokens per workgroup times compute units, the same for 64 and 128 dims.  Step without the launch ahead / with it, 8 KV
+// heads; append without rotation, 38 k of them 70.4 / 67.9 us (128 dims), 48 k 43.6 / 44.1 and 26.8 / 27.6 (64 dims), 77 k 43.5 / 45.8, 19.8 / 21.1 and 26.5 / 28.7;
+// with it, 77 k 71.8 / 68.6 and 43.5 / 41.2, 96 k 136.9 / 139.8 (64 CUs), 32.9 / 32.3 (128 CUs) and 75.5 / 75.0, 120 k 91.4 / 94.2 and 50.5 / 52.0, 192 k 48.6 / 51.4.
+static bool gqa_fp8_prepares(int64_t tokens, int n_wgs, int share, bool rope) { return tokens / n_wgs * share <= (rope ? 96 << 10 : 44 << 10); }
 
 // noalloc: the variant that allocates nothing.  The metadata's device twin and the workspace lie in the static scratch
 // array, the staging ring is used as spd_ctx_create made it, no timing events are recorded.
@@ -411,7 +418,7 @@ static int decode_step_impl(spd_ctx* ctx, spd_pool* pool, const spd_decode_batch
   if (ctx->device < 0) return SPD_ESTATE;
 
   const int B = b->n_req;
-  const bool mla = !gqa_kind(g.kind);
+  const bool mla = !gqa_kind(g.kind), eight = g.kind == SPD_KV_GQA_FP8;
   const int units_per_page = g.P / TILE_T;
   int64_t sum_units = 0;
   int32_t max_units = 0, max_pages = 0;
@@ -436,7 +443,7 @@ static int decode_step_impl(spd_ctx* ctx, spd_pool* pool, const spd_decode_batch
   const size_t w_bytes = b->rope ? sizeof(double) * (size_t)(b->rope->rotary_dim / 2) : 0;
   const int cut = ctx->env_decode_chunk_tiles;
   const int64_t cost = g.kind == SPD_KV_MLA_LATENT_FP8 ? CHUNK_COST_FP8 : CHUNK_COST;
-  if (!mla) split_gqa(ds, b->ctx_lens, B, sum_units, max_units, g.Hkv, share, cut, n_chunks.data(), sp, g.kind == SPD_KV_GQA_FP8 ? GQA_FP8_PER_CU : GQA_PER_CU);
+  if (!mla) split_gqa(ds, b->ctx_lens, B, sum_units, max_units, g.Hkv, share, cut, n_chunks.data(), sp, eight ? GQA_FP8_PER_CU : GQA_PER_CU);
   else if (!noalloc) split_latent(ds, b->ctx_lens, B, sum_units, share, units_per_page, cut, 0, n_chunks.data(), sp, cost);
   else
     split_latent_within_limits(ds, b->ctx_lens, B, b->n_q_heads, g.dv, sum_units, max_pages, share, units_per_page, cut, append, w_bytes,
@@ -454,15 +461,16 @@ static int decode_step_impl(spd_ctx* ctx, spd_pool* pool, const spd_decode_batch
   // Few workgroups read their records straight out of the pinned staging buffer: a launch less.  Above 128 KiB, as the
   // workgroups read them, they are copied too (a latent pool's workgroups, at most two per compute unit, are served as well from
   // pinned memory up to there: 2048 records on 128 CUs 155 us, 159 copied).
-  const bool many = !mla && gqa_many(n_wgs, share, g.dk);
+  const bool many = !mla && gqa_many(n_wgs, share, g.dk, eight);
   bool twin = many || (size_t)n_items * g.Hkv * stride > 131072;
   bool prepare = many && (append || b->rope) &&
-                 gqa_prepares(sum_units * g.Hkv * (int64_t)g.tile_bytes, n_wgs, share, b->rope != nullptr);
+                 (eight ? gqa_fp8_prepares(sum_units * g.Hkv * (int64_t)TILE_T, n_wgs, share, b->rope != nullptr)
+                        : gqa_prepares(sum_units * g.Hkv * (int64_t)g.tile_bytes, n_wgs, share, b->rope != nullptr));
   if (noalloc && bytes > NOALLOC_TWIN_BYTES) twin = prepare = false;
   // Split-K partials of a GQA launch of few workgroups are merged by that launch, where a request has few chunks; else by a
   // launch of its own.  Whole step over 128-dim heads, in the launch / on its own: 24 workgroups, 3 chunks 9.1 / 10.9 us; 192, 9
   // chunks 11.4 / 12.2 on 128 CUs; 400, 9 chunks 14.1 / 15.1 on 256; level from 500 to 1100 workgroups; 1392, 16 chunks 51.0 / 48.0
-  // (each workgroup pays for going past the L2).  Never for latent pools: their partials are four times as long, and the one
+  // (each workgroup pays for going past the L2).  Pages in 8 bits: 400 to 616 workgroups of 2 .. 4 chunks level, or 1 us shorter in the launch.  Never for latent pools: their partials are four times as long, and the one
   // workgroup that merges a request's 16 heads was 7 to 19 us at it (1 request of 4000 tokens in 16 chunks 39.6 / 20.4 us, 16 of 300
   // tokens 22.7 / 19.4).
   const bool inline_merge = !mla && n_wgs <= 512 && max_chunks <= MERGE_IN_LAUNCH_CHUNKS && (size_t)B * g.Hkv <= MERGE_COUNTERS;
