@@ -91,7 +91,8 @@ int spd_device_info(spd_ctx* ctx, int* total_cus, int* xcds, int* cu_granularity
  * GQA, 8 bits (the FP8 precision again; the format is this library's reading): the geometry of a GQA pool, but a cached row keeps OCP FP8 E4M3
  * codes, with one power-of-two scale for the keys and one for the values of each block: 16 consecutive positions (from a multiple of 16 on)
  * of one KV head.  The scale is the smallest 2^e, e >= -126, with which the block's largest finite magnitude does not pass 448, a code
- * is x / 2^e rounded to nearest even (infinities and NaN: NaN): 2 dim + 1/4 bytes per token and head instead of 4 dim.  Every call takes and
+ * is x / 2^e rounded to nearest even (infinities and NaN: NaN): 2 dim + 1/8 bytes per token and head instead of 4 dim; each page's scales are padded to
+ * a multiple of 128 bytes (pages of 16 tokens: 2 dim + 1 bytes with 8 heads, 2 dim + 8 with one).  Every call takes and
  * returns the same bf16 tensors as for a bf16 GQA pool.  spd_kv_gather hands back code * 2^e, which is exact in bf16, and the decode step attends
  * over those values.  Rows are written front to back: a write (spd_kv_write, a step's rows, an appended token) that begins at a
  * block's first position begins that block anew; one that begins further on keeps the block's rows ahead of it, under the larger of the block's
@@ -200,7 +201,9 @@ int spd_shm_kv_free_list(spd_shm_pool* pool, int32_t* out, int64_t cap, int64_t*
  * per-head tensors (n_kv_heads == n_q_heads, dim_qk 192, dim_v 128) and `latent` device
  * [T, 576] is what is written to the pages; latent must be NULL for a GQA pool.
  * Zero-length requests are SPD_EINVAL; scale must be positive and finite (the running maximum
- * of the scores is taken before scaling).
+ * of the scores is taken before scaling).  Scores and sums are fp32; softmax weights are rounded to bf16 for the
+ * product with v, and their sum is that of the rounded ones: besides its own rounding a result is off by up to
+ * 2^-7 sum p |v|, about twice what a decode step's is.
  *
  * Chunked prefill (paper, Evaluation "Baselines": the chunked-prefill variants): with
  * prefix_lens non-NULL (GQA pools, bf16 or 8 bits) request r already has prefix_lens[r] >= 0 tokens in its
@@ -252,7 +255,8 @@ int spd_prefill_step(spd_ctx* ctx, spd_pool* pool, const spd_prefill_batch* batc
  *        v_new NULL, out device [B, n_q_heads, 512];
  *        s[h,t] = scale * q[b,h,:] . c_t,  out[b,h,:] = sum_t softmax_t(s[h,:]) * c_t[0:512].
  * n_q_heads must be a multiple of n_kv_heads with at most 16 query heads per KV head; scale
- * must be positive and finite.
+ * must be positive and finite.  Scores and sums are fp32; on GQA pools softmax weights are rounded to bf16 for the product with
+ * the values, which is good for 2^-8 sum p |v| besides the result's own rounding.
  * With `rope` non-NULL (declared further down; paper, Evaluation "Implementation based on
  * DistServe": the RoPE kernel) q and k_new are the vectors BEFORE the rotary embedding: the step
  * rotates request b's query and new key by position ctx_lens[b] - 1, the key on its way into the page

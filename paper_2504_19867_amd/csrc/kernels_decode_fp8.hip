@@ -5,11 +5,11 @@
 // exact in bf16, so that the products are those of the values that codes and scales stand for, and the queries keep their bf16.
 //   S^T[key, query] = K_tile[16 x d] . Q^T[d x 16]       v_mfma_f32_16x16x32_bf16, d/32 steps for each of two tiles
 //   O^T[dim, query] += V^T[16 x 32] . P^T[32 x 16]       v_mfma_f32_16x16x32_bf16, d/16 blocks for both tiles together
-// Bound by memory: 2 d + 1/4 bytes per token and KV head.  A wave streams its tiles through two steps' registers, the scales of its next 64
+// Bound by memory: 2 d + 1/8 bytes per token and KV head.  A wave streams its tiles through two steps' registers, the scales of its next 64
 // tiles come by one load (one tile per lane) and from there by lane reads.  What is in registers bounds the workgroups of a compute unit, and
 // three with two steps hide one another's starts and ends better than two with four (64 requests of 512 .. 4096 tokens, 8 KV heads of 128 dims, on
 // 128 CUs 75.8 / 83.1 us, 128 lognormal ones of 64 query heads 139 / 147, six workgroups per compute unit dealt).  With two dealt (split_gqa) 69.4
-// and 137: 4.8 TB/s inside the attention launch, where a plain read through registers has 5.5; over bf16 pages 122 and 234.
+// and 137: 4.4 and 4.8 TB/s inside the attention launch, where a plain read through registers has 5.5; over bf16 pages 122 and 234.
 #include "decode_gqa.h"
 #include "gqa_fp8_tile.h"
 #include "internal.h"

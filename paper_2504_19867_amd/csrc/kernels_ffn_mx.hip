@@ -46,7 +46,8 @@ typedef unsigned int u32x4_any __attribute__((ext_vector_type(4), aligned(2))); 
 // ---- the packed weights.  A tile is 128 outputs x 128 hidden entries; unit u of it (16 outputs) keeps, from byte 2048 u on, the codes of its
 // gate rows, then of its up rows, [quarter of 32 entries][row][16 bytes], and from byte 16384 + 128 u on the scales, [row][gate, up][quarter].
 // Four lanes per (row, quarter), eight entries each: 16 lanes have the 256 bytes of a row that lie in the tile.  Bound by memory: hidden 4096, inter
-// 14336 (235 MB of bf16, 62 MB packed) 54 us packed and 52 unpacked on 256 CUs (5.5 and 5.7 TB/s), 77 and 73 on 128 (4 TB/s), 132 and 134 on 64.  A workgroup has
+// 14336 (235 MB of bf16, 62 MB packed) 54 us packed and 52 unpacked on 256 CUs (5.5 and 5.7 TB/s; event times of single
+// calls, which hold a launch each: back to back both together take 97), 77 and 73 on 128 (4 TB/s), 132 and 134 on 64.  A workgroup has
 // four groups of 256 pieces on their way, and finds its tile once for all its threads; with one piece per thread, each dividing for itself, 62 and 80, 103 and
 // 119, 178 and 225.  With a lane per (row, quarter), whose 64 bytes of bf16 are four accesses of its own: 80 and 97 on 256 CUs.
 constexpr int SCALES_AT = 16384;
